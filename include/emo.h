@@ -45,7 +45,8 @@
  * hipMalloc when a call needs more (waiting for the calls still using it) and is freed with
  * the handle, so steady-state calls allocate nothing and never block the host.  Since a
  * stream's buffer is found again by the stream's handle, a stream must have completed the
- * calls made on it before it is destroyed (a new stream may receive the same handle).
+ * calls made on it before it is destroyed (a new stream may receive the same handle).  The calls on
+ * logits take their workspace from the caller instead.
  *
  * Errors: every entry point returns an emo_status.  Argument errors that the host can detect
  * (sizes, null pointers, indices, non-finite or negative values, cycles, misaligned buffers)
@@ -368,6 +369,132 @@ emo_status emo_eval_intervals(emo_graph_t g, const uint8_t *levels, int64_t num_
  * disables); the caller owns them.  Not to be called while batch calls on `g` may run
  * concurrently on another thread. */
 emo_status emo_graph_set_timing_events(emo_graph_t g, void *begin_event, void *end_event);
+
+/*
+ * Proposing policies.  A learned or evolutionary search (the paper names both as the way for large
+ * graphs, Sec. VI-B) keeps a row of logits per pack, draws candidates from them, evaluates those, and
+ * moves the logits towards the best.  The calls below are its two ends: logits -> levels
+ * (emo_adjust_logits) and best candidates -> gradient (emo_distill_*).  They serve any rows of logits:
+ * the levels of a pack, the candidates of a batch (whose feasibility mask can be the mask here), a
+ * vocabulary.  No graph handle is involved; every operand is on the current device.
+ *
+ * An operand is an emo_tensor: element (r, c) is at data[r * row_stride + c * col_stride].  It may
+ * have fewer rows than the call: row r of the call reads row r % rows, and its rows must divide the
+ * call's (one row: shared by all; one per pack: repeated for every candidate).  Where "dense" is said
+ * col_stride must be 1 (any value with a single column); strides are >= 0, data is aligned to its
+ * element.  Outputs have exactly the call's rows, which must not overlap each other or any other
+ * operand, except that the adjusted logits or the gradient may be the logits themselves (same data,
+ * type, rows and strides).
+ * An operand passed as NULL is absent.  Data outside an operand's rows and columns (between strided
+ * rows, behind the last) is not written.
+ */
+typedef enum {
+    EMO_F32 = 0,
+    EMO_F16 = 1,
+    EMO_BF16 = 2,
+    EMO_U8 = 3,
+    EMO_I32 = 4,
+    EMO_I64 = 5
+} emo_dtype;
+
+typedef struct {
+    void *data;             /* device memory */
+    int64_t rows;
+    int64_t cols;
+    int64_t row_stride;     /* in elements */
+    int64_t col_stride;     /* in elements */
+    int32_t dtype;          /* emo_dtype */
+    int32_t reserved;       /* 0 */
+} emo_tensor;
+
+/*
+ * Logits with penalties for repeated entries, a bias, a temperature and a mask, and a choice from
+ * them.  For row r and entry v, with n the number of times v stands in the row's history:
+ *   x = logits[v]
+ *   n > 0:  x = x > 0 ? x / repetition : x * repetition
+ *           x = x - n * frequency
+ *           x = x - presence
+ *   x = x + bias[v];  x = x * inv_temperature;  x = -infinity where the mask's bit v is 0
+ * in fp32, every operation rounded by itself (no fused multiply-add), so the values are defined to the
+ * bit; steps whose operand is absent are left out.  A masked entry is -infinity whatever it held.
+ *   out[v] = x, rounded to out's type
+ *   choice = the lowest v of greatest x + noise[v] among the entries where that is > -infinity (a NaN
+ *            is never chosen; with Gumbel noise the choice is a draw from the row's softmax); -1 if
+ *            there is none, which in a byte is 255: a level that emo_evaluate takes for invalid.
+ *   rows            0 <= rows < 2^31; vocab: 1 <= V < 2^31.
+ *   logits          dense [.][V], EMO_F32, EMO_F16 or EMO_BF16.
+ *   history         [.][L] ids, EMO_U8, EMO_I32 or EMO_I64, any strides, 0 <= L < 2^31; ids outside
+ *                   [0, V) are ignored.  lengths: EMO_I32 [.][1] or NULL: only the first lengths[r]
+ *                   ids of a row count (clamped to [0, L]).  The three penalties need a history.
+ *   repetition, frequency, presence, inv_temperature: EMO_F32 [.][1].
+ *   bias, noise     dense [.][V], EMO_F32.
+ *   mask            dense [.][(V + 31) / 32], EMO_I32: bit v % 32 of word v / 32 is 1 where v is
+ *                   allowed (the layout of the feasibility masks).
+ *   out             dense [rows][V], the logits' type or EMO_F32, or NULL.
+ *   choice          [rows][1], EMO_U8 (V <= 255), EMO_I32 or EMO_I64, or NULL.
+ *   workspace       device memory of at least the bytes emo_adjust_workspace names for this rows and
+ *                   vocab, 16-byte aligned (NULL where that is 0).  Its contents before and after do
+ *                   not matter, but calls that may overlap (on two streams, or in two captured
+ *                   graphs) need one each.
+ * Asynchronous on `stream`, allocates nothing and may be captured.
+ */
+emo_status emo_adjust_logits(int64_t rows, int64_t vocab, const emo_tensor *logits,
+                             const emo_tensor *history, const emo_tensor *lengths,
+                             const emo_tensor *repetition, const emo_tensor *frequency,
+                             const emo_tensor *presence, const emo_tensor *bias,
+                             const emo_tensor *inv_temperature, const emo_tensor *mask,
+                             const emo_tensor *noise, const emo_tensor *out, const emo_tensor *choice,
+                             void *workspace, int64_t workspace_bytes, void *stream);
+emo_status emo_adjust_workspace(int64_t rows, int64_t vocab, int64_t *bytes);
+
+/*
+ * Distillation of rows of logits x from a teacher's top entries (ids with logits t), at a temperature:
+ * the cross entropy of the student's softmax against the teacher's over the listed entries.
+ *   p_k  = softmax of t_k / temperature over the row's valid entries: 0 <= id_k < V, id_k allowed by
+ *          the mask, t_k not -infinity; the rest (padding) do not count.  An id may stand in a row
+ *          several times (the levels of the best candidates do): its probabilities add up.
+ *   q_v  = softmax of x_v / temperature over the allowed entries
+ *   loss = -temperature^2 * sum over k of p_k log q_{id_k}         (terms with p_k = 0 are 0)
+ *   gradient[v] = scale * temperature * (q_v - sum of p_k over k with id_k = v), 0 where masked:
+ *          scale times the loss's derivative by x_v.
+ * The loss is the Kullback-Leibler divergence plus the teacher's entropy, which does not depend on x.
+ * A row without a valid entry has loss 0 and gradient 0 whatever its logits are; masked logits are not
+ * looked at.  In a row with valid entries a NaN or +infinity among the allowed logits or valid t_k
+ * makes the loss NaN, and the gradient wherever the formula does; so do allowed logits that are all
+ * -infinity.
+ * Sums are held in fp32, in a fixed order: the same call gives the same bits.
+ *   rows         0 <= N < 2^31; vocab: 1 <= V < 2^31; temperature finite and > 0.
+ *   logits       dense [N][V] (all N rows), EMO_F32, EMO_F16 or EMO_BF16.
+ *   ids          [.][K], 0 <= K <= 1024, EMO_U8, EMO_I32 or EMO_I64, any strides (level bytes
+ *                [K][P] serve as [P][K] with row_stride 1).
+ *   teacher      [.][K], EMO_F32, EMO_F16 or EMO_BF16, any strides.
+ *   mask         as in emo_adjust_logits, or NULL.
+ *   loss         EMO_F32 [N][1].
+ *   stats        EMO_F32 dense [N][2]: the greatest allowed logit m and the sum of exp((x_v - m) /
+ *                temperature) (-infinity and 0 if none is allowed): what emo_distill_backward needs of
+ *                the forward pass.
+ *   scale        EMO_F32 [.][1] or NULL (1): the derivative of the final loss by the row's loss.
+ *   gradient     dense [N][V], the logits' type or EMO_F32.
+ *   workspace    as in emo_adjust_logits, by emo_distill_workspace.
+ * emo_distill_forward gives loss and stats (either may be NULL), emo_distill_backward the gradient from
+ * stats (same logits, ids, teacher, temperature and mask as the forward pass), emo_distill_step loss
+ * (may be NULL) and gradient in one call, for a scale that is known beforehand.
+ * Asynchronous on `stream`, allocate nothing and may be captured.
+ */
+emo_status emo_distill_forward(int64_t rows, int64_t vocab, const emo_tensor *logits,
+                               const emo_tensor *ids, const emo_tensor *teacher, float temperature,
+                               const emo_tensor *mask, const emo_tensor *loss, const emo_tensor *stats,
+                               void *workspace, int64_t workspace_bytes, void *stream);
+emo_status emo_distill_backward(int64_t rows, int64_t vocab, const emo_tensor *logits,
+                                const emo_tensor *stats, const emo_tensor *ids,
+                                const emo_tensor *teacher, float temperature, const emo_tensor *scale,
+                                const emo_tensor *mask, const emo_tensor *gradient, void *stream);
+emo_status emo_distill_step(int64_t rows, int64_t vocab, const emo_tensor *logits,
+                            const emo_tensor *ids, const emo_tensor *teacher, float temperature,
+                            const emo_tensor *scale, const emo_tensor *mask, const emo_tensor *loss,
+                            const emo_tensor *gradient, void *workspace, int64_t workspace_bytes,
+                            void *stream);
+emo_status emo_distill_workspace(int64_t rows, int64_t vocab, int64_t *bytes);
 
 /*
  * Near-optimal policy search (Alg. 2, Sec. IV-F) with one frequency interval per pack, on the

@@ -25,7 +25,8 @@ ENTRY_POINTS = ("emo_load_graph", "emo_free_graph", "emo_graph_get_info",
                 "emo_eval_policies", "emo_slack", "emo_select_policy", "emo_evaluate", "emo_evaluate_targets",
                 "emo_select_from_results", "emo_select_from_results_noalloc", "emo_dp_search", "emo_eval_intervals",
                 "emo_graph_set_timing_events", "emo_pack_kernels", "emo_contract_packs",
-                "emo_pack_model",
+                "emo_pack_model", "emo_adjust_logits", "emo_adjust_workspace", "emo_distill_forward",
+                "emo_distill_backward", "emo_distill_step", "emo_distill_workspace",
                 "emo_graph_specialized_source", "emo_graph_node_source",
                 "emo_graph_segmented_source", "emo_graph_cut_source", "emo_graph_interval_source",
                 "emo_status_string",
@@ -54,6 +55,13 @@ class GraphInfo(ctypes.Structure):
 
     def as_dict(self):
         return {k: getattr(self, k) for k, _ in self._fields_}
+
+
+class Tensor(ctypes.Structure):
+    """emo_tensor: an operand of the calls on logits."""
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("col_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 KERNELS_AUTO, KERNELS_INTERPRETED, KERNELS_SPECIALIZED = 0, 1, 2
@@ -91,6 +99,12 @@ def _load_library():
         "emo_graph_set_timing_events": [P, P, P],
         "emo_pack_kernels": [i32, i32, P, P, P, P, P, i32, i32, P, f32, P, P],
         "emo_pack_model": [i32, i32, P, i32, P, P, i32, P, P, P, P, i32],
+        "emo_adjust_logits": [i64, i64] + [P] * 13 + [i64, P],
+        "emo_adjust_workspace": [i64, i64, P],
+        "emo_distill_forward": [i64, i64, P, P, P, f32, P, P, P, P, i64, P],
+        "emo_distill_backward": [i64, i64, P, P, P, P, f32, P, P, P, P],
+        "emo_distill_step": [i64, i64, P, P, P, f32, P, P, P, P, P, i64, P],
+        "emo_distill_workspace": [i64, i64, P],
         "emo_contract_packs": [i32, i32, P, P, P, P, i32, i32, P, P, P, i32, P, P, P, P, P, P,
                                P, P],
     }
@@ -392,6 +406,157 @@ def select_from_results_noalloc(makespan, energy, latency_target: float, mask, r
         float(latency_target), _dptr(mask, torch.int32, (B + 31) // 32, "mask"),
         _dptr(result, torch.int64, 3, "result"), _stream(stream)))
     return result, mask
+
+
+_DTYPES: dict = {}      # torch type -> emo_dtype
+
+
+def _operand(t, name: str, device, column: bool = False):
+    """emo_tensor of a device tensor [rows, n]; a 1-D tensor is one row, or with `column` one value
+    per row.  None stays None."""
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the logits are on {device}")
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
+                        torch.int64: 5})
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise ValueError(f"{name} has the type {t.dtype}, which no call takes")
+    shape, stride = t.shape, t.stride()
+    if column:
+        if len(shape) != 1:
+            raise ValueError(f"{name} must be [rows], one value per row")
+        return Tensor(t.data_ptr(), shape[0], 1, stride[0], 1, dtype, 0)
+    if len(shape) == 2:
+        return Tensor(t.data_ptr(), shape[0], shape[1], stride[0], stride[1], dtype, 0)
+    if len(shape) == 1:
+        return Tensor(t.data_ptr(), 1, shape[0], 0, stride[0], dtype, 0)
+    raise ValueError(f"{name} must have one or two dimensions")
+
+
+def _logits_shape(logits):
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, entries]")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    return int(logits.shape[0]), int(logits.shape[1])
+
+
+def _on_device(device, stream, call):
+    """Runs call(stream handle) with `device` current."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(device):
+        return call(_stream(stream))
+
+
+def _workspace(given, size_call, rows: int, vocab: int, device, stream):
+    """(pointer, bytes, tensor) of the workspace a call needs: the given one, or one allocated here
+    for the stream the call runs on (so that a captured call owns it)."""
+    import torch
+    n = ctypes.c_int64(0)
+    _check(size_call(rows, vocab, ctypes.byref(n)))
+    if given is None and n.value:
+        with torch.cuda.stream(stream):     # None: the current stream
+            given = torch.empty(n.value, dtype=torch.uint8, device=device)
+    if given is None:
+        return None, 0, None
+    if given.device != device or not given.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the logits' device")
+    return ctypes.c_void_p(given.data_ptr()), given.numel() * given.element_size(), given
+
+
+def _ref(t):
+    return None if t is None else ctypes.byref(t)
+
+
+def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None, repetition=None,
+                  frequency=None, presence=None, bias=None, inv_temperature=None, mask=None, noise=None,
+                  out=None, choice=None, workspace=None, stream=None):
+    """Penalties, bias, temperature and mask on rows of logits, and a choice from them
+    (emo_adjust_logits).  Returns (out, choice): what was given; the adjusted logits are allocated
+    (in the logits' type) when neither is.
+
+    logits [n, V]; history [n, L] ids; lengths, repetition, frequency, presence, inv_temperature [n];
+    bias, noise [n, V] or [V]; mask [n, (V + 31) // 32] or one row, int32 words; out [rows, V]; choice
+    [rows] uint8, int32 or int64.  Row r reads row r % n of each; rows defaults to the logits' n."""
+    import torch
+    n, V = _logits_shape(logits)
+    rows = n if rows is None else int(rows)
+    dev = logits.device
+    if out is None and choice is None:
+        with torch.cuda.stream(stream):
+            out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
+    args = [_operand(logits, "logits", dev), _operand(history, "history", dev), _operand(lengths, "lengths", dev, True),
+            _operand(repetition, "repetition", dev, True), _operand(frequency, "frequency", dev, True),
+            _operand(presence, "presence", dev, True), _operand(bias, "bias", dev),
+            _operand(inv_temperature, "inv_temperature", dev, True), _operand(mask, "mask", dev),
+            _operand(noise, "noise", dev), _operand(out, "out", dev), _operand(choice, "choice", dev, True)]
+    ws, size, _keep = (None, 0, None) if choice is None else \
+        _workspace(workspace, lib.emo_adjust_workspace, rows, V, dev, stream)
+    _check(_on_device(dev, stream, lambda st: lib.emo_adjust_logits(rows, V, *map(_ref, args), ws, size, st)))
+    return out, choice
+
+
+def distill_forward(logits, ids, teacher, temperature: float = 1.0, *, mask=None, loss=None, stats=None,
+                    workspace=None, stream=None):
+    """Cross entropy of the logits [N, V] against a teacher's top entries (emo_distill_forward):
+    ids [n, K], teacher [n, K] or one row each.  Returns (loss [N], stats [N, 2] for the backward
+    pass), allocated when not given.  Autograd does not see it: distill_backward is the gradient."""
+    import torch
+    N, V = _logits_shape(logits)
+    dev = logits.device
+    with torch.cuda.stream(stream):
+        loss = torch.empty(N, dtype=torch.float32, device=dev) if loss is None else loss
+        stats = torch.empty((N, 2), dtype=torch.float32, device=dev) if stats is None else stats
+    args = [_operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev)]
+    outs = [_operand(mask, "mask", dev), _operand(loss, "loss", dev, True), _operand(stats, "stats", dev)]
+    ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, dev, stream)
+    _check(_on_device(dev, stream, lambda st: lib.emo_distill_forward(
+        N, V, *map(_ref, args), float(temperature), *map(_ref, outs), ws, size, st)))
+    return loss, stats
+
+
+def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, grad=None,
+                     stream=None):
+    """Gradient [N, V] of sum(scale * loss) by the logits, from the statistics that distill_forward
+    returned for the same operands (emo_distill_backward); scale [n] or None (1).  `grad` may be the
+    logits."""
+    import torch
+    N, V = _logits_shape(logits)
+    dev = logits.device
+    if grad is None:
+        with torch.cuda.stream(stream):
+            grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    args = [_operand(logits, "logits", dev), _operand(stats, "stats", dev), _operand(ids, "ids", dev),
+            _operand(teacher, "teacher", dev)]
+    outs = [_operand(scale, "scale", dev, True), _operand(mask, "mask", dev), _operand(grad, "grad", dev)]
+    _check(_on_device(dev, stream, lambda st: lib.emo_distill_backward(
+        N, V, *map(_ref, args), float(temperature), *map(_ref, outs), st)))
+    return grad
+
+
+def distill_step(logits, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, loss=None, grad=None,
+                 workspace=None, stream=None):
+    """Loss [N] and gradient [N, V] in one call (emo_distill_step), for a scale known beforehand (e.g.
+    [1 / N]).  `grad` may be the logits."""
+    import torch
+    N, V = _logits_shape(logits)
+    dev = logits.device
+    with torch.cuda.stream(stream):
+        loss = torch.empty(N, dtype=torch.float32, device=dev) if loss is None else loss
+        grad = torch.empty((N, V), dtype=logits.dtype, device=dev) if grad is None else grad
+    args = [_operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev)]
+    outs = [_operand(scale, "scale", dev, True), _operand(mask, "mask", dev), _operand(loss, "loss", dev, True),
+            _operand(grad, "grad", dev)]
+    ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, dev, stream)
+    _check(_on_device(dev, stream, lambda st: lib.emo_distill_step(
+        N, V, *map(_ref, args), float(temperature), *map(_ref, outs), ws, size, st)))
+    return loss, grad
 
 
 def unpack_mask(mask, B: int) -> np.ndarray:
