@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(DistillArgs a) {
             m = st[0];
             s = st[1];
         }
-        const uint32_t irow = K ? r % a.ids.rows : 0, trow = K ? r % a.teacher.rows : 0;
+        const uint32_t irow = row_index(a.ids, r), trow = row_index(a.teacher, r);
         float tm = -INFINITY;
         float any = 0.f;
         for (int k = tid; k < K; k += kThreads) {

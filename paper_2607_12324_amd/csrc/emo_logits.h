@@ -17,13 +17,22 @@ struct Mat {
     const char *data;
     int64_t row_stride, col_stride;   // elements
     uint32_t rows;
+    uint32_t magic, shift;            // r / rows = mulhi(r, magic) >> shift; magic 0: see row_index
     int32_t cols;
     int32_t dtype;
 };
 
+// The operand's row that row r < 2^31 of the call reads.  With magic 0 that is r itself: the operand has
+// all rows, or one with a row stride of 0.  A remainder by the compiler's division takes about 20
+// instructions an operand, which bounded rows of a few entries.
+__device__ __forceinline__ uint32_t row_index(const Mat &m, uint32_t r) {
+    if (m.magic == 0) return r;
+    return r - (__umulhi(r, m.magic) >> m.shift) * m.rows;
+}
+
 template <typename T>
 __device__ __forceinline__ const T *row_of(const Mat &m, uint32_t r) {
-    return reinterpret_cast<const T *>(m.data) + static_cast<int64_t>(r % m.rows) * m.row_stride;
+    return reinterpret_cast<const T *>(m.data) + static_cast<int64_t>(row_index(m, r)) * m.row_stride;
 }
 
 __device__ __forceinline__ float row_value(const Mat &m, uint32_t r, float absent) {
@@ -45,6 +54,98 @@ __device__ __forceinline__ float load_float(const Mat &m, uint32_t row, int32_t 
     if (m.dtype == EMO_F32) return reinterpret_cast<const float *>(m.data)[at];
     if (m.dtype == EMO_F16) return static_cast<float>(reinterpret_cast<const _Float16 *>(m.data)[at]);
     return static_cast<float>(reinterpret_cast<const __bf16 *>(m.data)[at]);
+}
+
+// Entries of a row that a lane holds at once: 16 bytes of logits, loaded at any alignment of the type (rows
+// of an odd count start anywhere; the hardware takes 16-byte accesses at such addresses).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2), may_alias));
+template <typename T>
+constexpr int kChunk = 16 / sizeof(T);
+
+template <typename T>
+__device__ __forceinline__ float entry(u32x4 raw, int j);
+template <>
+__device__ __forceinline__ float entry<float>(u32x4 raw, int j) { return __uint_as_float(raw[j]); }
+template <>
+__device__ __forceinline__ float entry<_Float16>(u32x4 raw, int j) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(raw[j >> 1] >> (j & 1) * 16)));
+}
+template <>
+__device__ __forceinline__ float entry<__bf16>(u32x4 raw, int j) {
+    return __uint_as_float(j & 1 ? raw[j >> 1] & 0xffff0000u : raw[j >> 1] << 16);
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t bits_of(float x) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(x);
+    else return __builtin_bit_cast(uint16_t, static_cast<T>(x));
+}
+
+// The chunk at entry v of a row of V; entries from V on are -infinity.
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T *row, int64_t v, int32_t V) {
+    constexpr int N = kChunk<T>;
+    if (v + N <= V) return *reinterpret_cast<const u32x4_any *>(row + v);
+    const uint32_t none = bits_of<T>(-INFINITY);
+    u32x4 raw;
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (N == 4) {
+            raw[w] = v + w < V ? reinterpret_cast<const uint32_t *>(row)[v + w] : none;
+        } else {
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(row);
+            const uint32_t lo = v + 2 * w < V ? p[v + 2 * w] : none;
+            const uint32_t hi = v + 2 * w + 1 < V ? p[v + 2 * w + 1] : none;
+            raw[w] = lo | hi << 16;
+        }
+    }
+    return raw;
+}
+
+// N floats at entry v of a row of V (zeros from V on).
+template <int N>
+__device__ __forceinline__ void load_floats(const float *row, int64_t v, int32_t V, float (&f)[N]) {
+    if (v + N <= V) {
+        for (int i = 0; i < N; i += 4) {
+            const u32x4 raw = *reinterpret_cast<const u32x4_any *>(row + v + i);
+            for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(raw[j]);
+        }
+    } else {
+        for (int j = 0; j < N; ++j) f[j] = v + j < V ? row[v + j] : 0.f;
+    }
+}
+
+// N values at entry v of a row of V, each rounded once to the row's type.
+template <typename O, int N>
+__device__ __forceinline__ void store_chunk(O *row, int64_t v, int32_t V, const float (&f)[N]) {
+    if (v + N <= V) {
+        if constexpr (sizeof(O) == 4) {
+            for (int i = 0; i < N; i += 4) {
+                u32x4 raw;
+                for (int j = 0; j < 4; ++j) raw[j] = __float_as_uint(f[i + j]);
+                *reinterpret_cast<u32x4_any *>(row + v + i) = raw;
+            }
+        } else if constexpr (N == 4) {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            const u32x2 raw = {bits_of<O>(f[0]) | bits_of<O>(f[1]) << 16, bits_of<O>(f[2]) | bits_of<O>(f[3]) << 16};
+            *reinterpret_cast<u32x2_any *>(row + v) = raw;
+        } else {
+            u32x4 raw;
+            for (int w = 0; w < 4; ++w) raw[w] = bits_of<O>(f[2 * w]) | bits_of<O>(f[2 * w + 1]) << 16;
+            *reinterpret_cast<u32x4_any *>(row + v) = raw;
+        }
+    } else {
+        for (int j = 0; j < N; ++j)
+            if (v + j < V) row[v + j] = static_cast<O>(f[j]);
+    }
+}
+
+// The mask's bits of the N entries from v on, a multiple of N (N 4 or 8): a row's words are read by the byte.
+template <int N>
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t *mask, int64_t v) {
+    if (!mask) return (1u << N) - 1;
+    return (reinterpret_cast<const uint8_t *>(mask)[v >> 3] >> (v & 7)) & ((1u << N) - 1);
 }
 
 __device__ __forceinline__ bool allowed(const uint32_t *mask, int32_t v) {
@@ -129,6 +230,15 @@ struct Checker {
         m.row_stride = t->row_stride;
         m.col_stride = t->col_stride;
         m.dtype = t->dtype;
+        if (t->rows == 1) {
+            m.row_stride = 0;
+        } else if (t->rows != rows) {
+            // 2 <= n < 2^31, s = the least with n <= 2^s: r * (2^(31 + s) / n + 1) >> (31 + s) is r / n for r < 2^31
+            int bits = 1;
+            while ((int64_t(1) << bits) < t->rows) ++bits;
+            m.magic = static_cast<uint32_t>((static_cast<unsigned __int128>(1) << (31 + bits)) / static_cast<uint64_t>(t->rows) + 1);
+            m.shift = static_cast<uint32_t>(bits - 1);
+        }
         if (t->cols == 0) return m;
         if (!t->data) return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s has no data", name)), m;
         const int64_t size = size_of(t->dtype);

@@ -17,7 +17,6 @@ struct AdjustArgs {
     int32_t choice_dtype;
 };
 
-constexpr int kTile = 4096;     // entries whose counts lie in LDS at once
 
 struct Best {
     float value;
@@ -47,80 +46,181 @@ __device__ __forceinline__ void store_choice(const AdjustArgs &a, uint32_t r, Be
     else reinterpret_cast<int64_t *>(a.choice)[at] = c;
 }
 
-// A workgroup per row, tile after tile: the history's ids in the tile are counted in LDS (integer
-// atomics: any order gives the same counts), then every entry goes through the formula once.
-template <typename T, typename O>
-__global__ void __launch_bounds__(kThreads) adjust_row_kernel(AdjustArgs a) {
-    __shared__ uint32_t s_count[kTile];
-    __shared__ Best s_best[kThreads / 64];
+// A workgroup's best entry, valid in thread 0.
+template <int Threads>
+__device__ __forceinline__ Best block_best(Best b) {
+    b = wave_best(b);
+    if constexpr (Threads > 64) {
+        __shared__ Best s_best[Threads / 64];
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) s_best[threadIdx.x / 64] = b;
+        __syncthreads();
+        for (int w = 0; w < Threads / 64; ++w) b = better(b, s_best[w]);
+    }
+    return b;
+}
+
+// What the steps need of a row.
+struct RowRates {
+    float repetition, frequency, presence, inv_temperature;
+};
+
+__device__ __forceinline__ RowRates rates_of(const AdjustArgs &a, uint32_t r) {
+    return {row_value(a.repetition, r, 1.f), row_value(a.frequency, r, 0.f), row_value(a.presence, r, 0.f),
+            row_value(a.inv_temperature, r, 1.f)};
+}
+
+// Adjusts N entries (x) that the history holds n times, and keeps the best for the choice.
+template <int N>
+__device__ __forceinline__ void adjust_entries(const AdjustArgs &a, const RowRates &rate, float (&x)[N], const uint32_t (&n)[N],
+                                               bool penalties, const float (&bias)[N], const float (&noise)[N], uint32_t bits,
+                                               int32_t v, Best &best) {
+    if (penalties) {
+        for (int j = 0; j < N; ++j) {
+            if (n[j] == 0) continue;
+            if (a.repetition.data) x[j] = x[j] > 0.f ? x[j] / rate.repetition : x[j] * rate.repetition;
+            if (a.frequency.data) x[j] = x[j] - static_cast<float>(n[j]) * rate.frequency;
+            if (a.presence.data) x[j] = x[j] - rate.presence;
+        }
+    }
+    for (int j = 0; j < N; ++j) {
+        if (a.bias.data) x[j] = x[j] + bias[j];
+        if (a.inv_temperature.data) x[j] = x[j] * rate.inv_temperature;
+        if (!(bits >> j & 1)) x[j] = -INFINITY;
+        const float y = a.noise.data ? x[j] + noise[j] : x[j];
+        if (y > best.value && x[j] > -INFINITY) best = {y, v + j};
+    }
+}
+
+__device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r) {
+    if (!a.history.data) return 0;
+    const int32_t L = a.history.cols;
+    return a.lengths.data ? min(max(*row_of<int32_t>(a.lengths, r), 0), L) : L;
+}
+
+constexpr int kPerThread = 32;      // entries a thread holds
+
+// A workgroup per tile of Threads * 32 entries of a row.  Bound by memory: a thread's logits (64 or 128
+// bytes) are all in flight before anything else; while they come, the history's ids in the tile are
+// counted in LDS (4 bytes an entry; integer atomics: any order gives the same counts).  The choice of a
+// row of several tiles goes through `parts`, one best entry a tile, and choose_kernel.
+template <typename T, typename O, int Threads, bool History>
+__global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, int32_t tiles, Best *parts) {
+    constexpr int N = kChunk<T>, C = kPerThread / N, Tile = Threads * kPerThread;
+    __shared__ alignas(16) uint32_t s_count[History ? Tile : 4];
     const int tid = threadIdx.x;
-    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const int64_t blocks = static_cast<int64_t>(a.rows) * tiles;
+    for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+        const uint32_t r = static_cast<uint32_t>(tiles == 1 ? b : b / tiles);
+        const int64_t v0 = (b - static_cast<int64_t>(r) * tiles) * Tile;
         const T *logits = row_of<T>(a.logits, r);
         const float *bias = a.bias.data ? row_of<float>(a.bias, r) : nullptr;
         const float *noise = a.noise.data ? row_of<float>(a.noise, r) : nullptr;
         const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
-        const uint32_t hrow = a.history.data ? r % a.history.rows : 0;
-        int32_t L = a.history.data ? a.history.cols : 0;
-        if (a.lengths.data) L = min(max(*row_of<int32_t>(a.lengths, r), 0), L);
-        const float rep = row_value(a.repetition, r, 1.f);
-        const float freq = row_value(a.frequency, r, 0.f);
-        const float pres = row_value(a.presence, r, 0.f);
-        const float inv_t = row_value(a.inv_temperature, r, 1.f);
+        u32x4 raw[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int64_t v = v0 + (c * Threads + tid) * N;
+            if (v < a.vocab) raw[c] = load_chunk(logits, v, a.vocab);
+        }
+        const RowRates rate = rates_of(a, r);
+        const int32_t L = History ? live_history(a, r) : 0;
+        if (History && L > 0) {
+            const uint32_t hrow = row_index(a.history, r);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < Tile; i += 4 * Threads) *reinterpret_cast<u32x4 *>(&s_count[i + 4 * tid]) = u32x4{0, 0, 0, 0};
+            __syncthreads();
+            for (int32_t i = tid; i < L; i += Threads) {
+                const int64_t id = load_id(a.history, hrow, i, a.vocab) - v0;
+                if (id >= 0 && id < Tile) atomicAdd(&s_count[id], 1u);
+            }
+            __syncthreads();
+        }
         Best best = {-INFINITY, INT32_MAX};
-        for (int64_t v0 = 0; v0 < a.vocab; v0 += kTile) {
-            const int32_t n = static_cast<int32_t>(min(static_cast<int64_t>(kTile), a.vocab - v0));
-            if (L > 0) {
-                __syncthreads();
-                for (int i = tid; i < n; i += kThreads) s_count[i] = 0;
-                __syncthreads();
-                for (int32_t i = tid; i < L; i += kThreads) {
-                    const int64_t id = load_id(a.history, hrow, i, a.vocab) - v0;
-                    if (id >= 0 && id < n) atomicAdd(&s_count[id], 1u);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int e = (c * Threads + tid) * N;
+            const int64_t v = v0 + e;
+            if (v >= a.vocab) break;
+            float x[N], bs[N], ns[N];
+            uint32_t n[N];
+            if (bias) load_floats(bias, v, a.vocab, bs);
+            if (noise) load_floats(noise, v, a.vocab, ns);
+            const uint32_t bits = mask_bits<N>(mask, v);
+            for (int j = 0; j < N; ++j) x[j] = entry<T>(raw[c], j);
+            if (History && L > 0) {
+                for (int j = 0; j < N; j += 4) {
+                    const u32x4 q = *reinterpret_cast<const u32x4 *>(&s_count[e + j]);
+                    for (int i = 0; i < 4; ++i) n[j + i] = q[i];
                 }
-                __syncthreads();
             }
-            for (int i = tid; i < n; i += kThreads) {
-                const int32_t v = static_cast<int32_t>(v0 + i);
-                float x = static_cast<float>(logits[v]);
-                const uint32_t seen = L > 0 ? s_count[i] : 0;
-                if (seen) {
-                    if (a.repetition.data) x = x > 0.f ? x / rep : x * rep;
-                    if (a.frequency.data) x = x - static_cast<float>(seen) * freq;
-                    if (a.presence.data) x = x - pres;
-                }
-                if (bias) x = x + bias[v];
-                if (a.inv_temperature.data) x = x * inv_t;
-                if (!allowed(mask, v)) x = -INFINITY;
-                if (a.out) reinterpret_cast<O *>(a.out)[static_cast<int64_t>(r) * a.out_stride + v] = static_cast<O>(x);
-                const float y = noise ? x + noise[v] : x;
-                if (y > best.value && x > -INFINITY) best = {y, v};
-            }
+            adjust_entries(a, rate, x, n, History && L > 0, bs, ns, bits, static_cast<int32_t>(v), best);
+            if (a.out) store_chunk(reinterpret_cast<O *>(a.out) + static_cast<int64_t>(r) * a.out_stride, v, a.vocab, x);
         }
         if (a.choice) {
-            best = wave_best(best);
-            __syncthreads();
-            if (tid % 64 == 0) s_best[tid / 64] = best;
-            __syncthreads();
+            best = block_best<Threads>(best);
             if (tid == 0) {
-                for (int w = 1; w < kThreads / 64; ++w) best = better(best, s_best[w]);
-                store_choice(a, r, best);
+                if (tiles == 1) store_choice(a, r, best);
+                else parts[b] = best;
             }
-            __syncthreads();
         }
     }
 }
 
+// The choice of rows of several tiles, a workgroup per row.
+__global__ void __launch_bounds__(kThreads) choose_kernel(AdjustArgs a, int32_t tiles, const Best *parts) {
+    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        Best best = {-INFINITY, INT32_MAX};
+        for (int32_t t = threadIdx.x; t < tiles; t += kThreads) best = better(best, parts[static_cast<int64_t>(r) * tiles + t]);
+        best = block_best<kThreads>(best);
+        if (threadIdx.x == 0) store_choice(a, r, best);
+    }
+}
+
+// Tiles of a row: of 8,192 entries for workgroups of 256 threads while that gives work to every compute
+// unit (4 workgroups each), of 2,048 for single waves on shorter rows and for few rows.
+struct Tiling {
+    int threads;
+    int64_t tiles;
+};
+
+Tiling tiling(int64_t rows, int64_t vocab) {
+    const int64_t wide = (vocab + 8191) / 8192;
+    if (vocab > 2048 && rows * wide >= 1024) return {256, wide};
+    return {64, (vocab + 2047) / 2048};
+}
+
+unsigned blocks_for(int64_t n) { return static_cast<unsigned>(n < kMaxBlocks ? n : kMaxBlocks); }
+
 struct AdjustLaunch {
     const AdjustArgs &a;
+    Best *parts;
     hipStream_t st;
+
+    template <typename T, typename O, int Threads>
+    void tiles(int32_t n) const {
+        const dim3 grid(blocks_for(static_cast<int64_t>(a.rows) * n));
+        if (a.history.data)
+            hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, true>), grid, dim3(Threads), 0, st, a, n, parts);
+        else
+            hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, false>), grid, dim3(Threads), 0, st, a, n, parts);
+        if (a.choice && n > 1) hipLaunchKernelGGL(choose_kernel, dim3(blocks_for(a.rows)), dim3(kThreads), 0, st, a, n, parts);
+    }
+
     template <typename T, typename O>
     void run() const {
-        hipLaunchKernelGGL((adjust_row_kernel<T, O>), dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
+        const Tiling t = tiling(a.rows, a.vocab);
+        if (t.threads == 64) tiles<T, O, 64>(static_cast<int32_t>(t.tiles));
+        else tiles<T, O, 256>(static_cast<int32_t>(t.tiles));
     }
 };
 
-// Workspace bytes of a call.
-int64_t adjust_bytes(int64_t, int64_t) { return 0; }
+// Workspace bytes of a call: the best entry of every tile of rows of several.
+int64_t adjust_bytes(int64_t rows, int64_t vocab) {
+    const int64_t tiles = tiling(rows, vocab).tiles;
+    return tiles > 1 ? rows * tiles * static_cast<int64_t>(sizeof(Best)) : 0;
+}
 
 }  // namespace
 
@@ -169,7 +269,7 @@ emo_status emo_adjust_logits(int64_t rows, int64_t vocab, const emo_tensor *logi
     a.choice = const_cast<char *>(ch.data);
     a.choice_stride = ch.row_stride;
     a.choice_dtype = ch.dtype;
-    by_types(a.logits.dtype, out ? o.dtype : a.logits.dtype, AdjustLaunch{a, static_cast<hipStream_t>(stream)});
+    by_types(a.logits.dtype, out ? o.dtype : a.logits.dtype, AdjustLaunch{a, static_cast<Best *>(workspace), static_cast<hipStream_t>(stream)});
     return launched("emo_adjust_logits");
 }
 
