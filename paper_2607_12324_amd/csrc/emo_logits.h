@@ -103,6 +103,28 @@ __device__ __forceinline__ u32x4 load_chunk(const T *row, int64_t v, int32_t V) 
     return raw;
 }
 
+// Four entries at v of a row of V, as floats (-infinity from V on).
+template <typename T>
+__device__ __forceinline__ void load_four(const T *row, int32_t v, int32_t V, float (&x)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        const u32x4 raw = load_chunk(row, v, V);
+        for (int j = 0; j < 4; ++j) x[j] = entry<T>(raw, j);
+    } else {
+        u32x4 raw = {0, 0, 0, 0};
+        if (v + 4 <= V) {
+            const auto two = *reinterpret_cast<const u32x2_any *>(row + v);
+            raw[0] = two[0];
+            raw[1] = two[1];
+        } else {
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(row);
+            const uint32_t none = bits_of<T>(-INFINITY);
+            for (int w = 0; w < 2; ++w)
+                raw[w] = (v + 2 * w < V ? p[v + 2 * w] : none) | (v + 2 * w + 1 < V ? p[v + 2 * w + 1] : none) << 16;
+        }
+        for (int j = 0; j < 4; ++j) x[j] = entry<T>(raw, j);
+    }
+}
+
 // N floats at entry v of a row of V (zeros from V on).
 template <int N>
 __device__ __forceinline__ void load_floats(const float *row, int64_t v, int32_t V, float (&f)[N]) {

@@ -168,6 +168,49 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, int3
     }
 }
 
+// Rows of at most 64 entries: a group of 2^lg lanes per row, four entries a lane, so that a wave reads
+// neighbouring rows in one piece; the choice is a reduction within the group.  The history (short: see
+// small_rows) is compared entry by entry.
+template <typename T, typename O>
+__global__ void __launch_bounds__(kThreads) adjust_group_kernel(AdjustArgs a, int lg) {
+    const int lanes = 1 << lg;
+    const int64_t total = static_cast<int64_t>(a.rows) << lg;
+    for (int64_t b = static_cast<int64_t>(blockIdx.x) * kThreads; b < total; b += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t g = b + threadIdx.x;
+        const bool live = g < total;
+        const uint32_t r = static_cast<uint32_t>((live ? g : total - 1) >> lg);
+        const int32_t v = (threadIdx.x & (lanes - 1)) * 4;
+        Best best = {-INFINITY, INT32_MAX};
+        if (live && v < a.vocab) {
+            float x[4], bias[4], noise[4];
+            uint32_t n[4] = {0, 0, 0, 0};
+            if (a.noise.data) load_floats(row_of<float>(a.noise, r), v, a.vocab, noise);
+            load_four(row_of<T>(a.logits, r), v, a.vocab, x);
+            if (a.bias.data) load_floats(row_of<float>(a.bias, r), v, a.vocab, bias);
+            const uint32_t bits = mask_bits<4>(a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr, v);
+            const int32_t L = live_history(a, r);
+            if (L > 0) {
+                const uint32_t hrow = row_index(a.history, r);
+                for (int32_t i = 0; i < L; ++i) {
+                    const int32_t id = load_id(a.history, hrow, i, a.vocab) - v;
+                    for (int j = 0; j < 4; ++j) n[j] += id == j;
+                }
+            }
+            adjust_entries(a, rates_of(a, r), x, n, L > 0, bias, noise, bits, v, best);
+            if (a.out) store_chunk(reinterpret_cast<O *>(a.out) + static_cast<int64_t>(r) * a.out_stride, v, a.vocab, x);
+        }
+        if (a.choice) {
+            for (int off = lanes >> 1; off > 0; off >>= 1) {
+                Best o;
+                o.value = __shfl_xor(best.value, off, 64);
+                o.at = __shfl_xor(best.at, off, 64);
+                best = better(best, o);
+            }
+            if (live && v == 0) store_choice(a, r, best);
+        }
+    }
+}
+
 // The choice of rows of several tiles, a workgroup per row.
 __global__ void __launch_bounds__(kThreads) choose_kernel(AdjustArgs a, int32_t tiles, const Best *parts) {
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -178,8 +221,12 @@ __global__ void __launch_bounds__(kThreads) choose_kernel(AdjustArgs a, int32_t 
     }
 }
 
-// Tiles of a row: of 8,192 entries for workgroups of 256 threads while that gives work to every compute
+// A row's tiles: of 8,192 entries for workgroups of 256 threads while that gives work to every compute
 // unit (4 workgroups each), of 2,048 for single waves on shorter rows and for few rows.
+// Rows that a group of lanes takes: of at most 64 entries, with a history of at most 64 ids (each is
+// compared with every entry; longer ones are counted in LDS).
+bool small_rows(const AdjustArgs &a) { return a.vocab <= 64 && (!a.history.data || a.history.cols <= 64); }
+
 struct Tiling {
     int threads;
     int64_t tiles;
@@ -210,6 +257,13 @@ struct AdjustLaunch {
 
     template <typename T, typename O>
     void run() const {
+        if (small_rows(a)) {
+            int lg = 0;
+            while ((4 << lg) < a.vocab) ++lg;
+            const int64_t blocks = ((static_cast<int64_t>(a.rows) << lg) + kThreads - 1) / kThreads;
+            hipLaunchKernelGGL((adjust_group_kernel<T, O>), dim3(blocks_for(blocks)), dim3(kThreads), 0, st, a, lg);
+            return;
+        }
         const Tiling t = tiling(a.rows, a.vocab);
         if (t.threads == 64) tiles<T, O, 64>(static_cast<int32_t>(t.tiles));
         else tiles<T, O, 256>(static_cast<int32_t>(t.tiles));

@@ -412,16 +412,12 @@ _DTYPES: dict = {}      # torch type -> emo_dtype
 
 
 def _operand(t, name: str, device, column: bool = False):
-    """emo_tensor of a device tensor [rows, n]; a 1-D tensor is one row, or with `column` one value
-    per row.  None stays None."""
+    """emo_tensor of a device tensor [rows, n], by reference; a 1-D tensor is one row, or with
+    `column` one value per row.  None stays None."""
     if t is None:
         return None
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the logits are on {device}")
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
-                        torch.int64: 5})
     dtype = _DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{name} has the type {t.dtype}, which no call takes")
@@ -429,49 +425,65 @@ def _operand(t, name: str, device, column: bool = False):
     if column:
         if len(shape) != 1:
             raise ValueError(f"{name} must be [rows], one value per row")
-        return Tensor(t.data_ptr(), shape[0], 1, stride[0], 1, dtype, 0)
+        return ctypes.byref(Tensor(t.data_ptr(), shape[0], 1, stride[0], 1, dtype, 0))
     if len(shape) == 2:
-        return Tensor(t.data_ptr(), shape[0], shape[1], stride[0], stride[1], dtype, 0)
+        return ctypes.byref(Tensor(t.data_ptr(), shape[0], shape[1], stride[0], stride[1], dtype, 0))
     if len(shape) == 1:
-        return Tensor(t.data_ptr(), 1, shape[0], 0, stride[0], dtype, 0)
+        return ctypes.byref(Tensor(t.data_ptr(), 1, shape[0], 0, stride[0], dtype, 0))
     raise ValueError(f"{name} must have one or two dimensions")
 
 
 def _logits_shape(logits):
-    if logits.dim() != 2:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
+                        torch.int64: 5})
+    shape = logits.shape
+    if len(shape) != 2:
         raise ValueError("logits must be [rows, entries]")
     if not logits.is_cuda:
         raise ValueError("logits must be a device tensor")
-    return int(logits.shape[0]), int(logits.shape[1])
+    return shape[0], shape[1], logits.device
 
 
-def _on_device(device, stream, call):
-    """Runs call(stream handle) with `device` current."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        return call(_stream(stream))
-    with torch.cuda.device(device):
-        return call(_stream(stream))
+class _Place:
+    """Where a call on logits runs: their device made current, and a stream of it (the current one, or
+    the one given).  Tensors that the call makes belong to that stream, so a captured call owns its
+    workspace and a reused one is free of the calls before it."""
 
+    def __init__(self, device, stream):
+        import torch
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the logits are on {device}")
+        self._torch, self.device, self._guard = torch, device, None
+        if stream is not None:
+            self._guard = torch.cuda.stream(stream)
+        elif device.index != torch.cuda.current_device():
+            self._guard = torch.cuda.device(device)
 
-def _workspace(given, size_call, rows: int, vocab: int, device, stream):
-    """(pointer, bytes, tensor) of the workspace a call needs: the given one, or one allocated here
-    for the stream the call runs on (so that a captured call owns it)."""
-    import torch
-    n = ctypes.c_int64(0)
-    _check(size_call(rows, vocab, ctypes.byref(n)))
-    if given is None and n.value:
-        with torch.cuda.stream(stream):     # None: the current stream
-            given = torch.empty(n.value, dtype=torch.uint8, device=device)
-    if given is None:
-        return None, 0, None
-    if given.device != device or not given.is_contiguous():
-        raise ValueError("workspace must be contiguous and on the logits' device")
-    return ctypes.c_void_p(given.data_ptr()), given.numel() * given.element_size(), given
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+        return self
 
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
 
-def _ref(t):
-    return None if t is None else ctypes.byref(t)
+    def empty(self, shape, dtype=None):
+        return self._torch.empty(shape, dtype=dtype or self._torch.float32, device=self.device)
+
+    def workspace(self, given, size_call, rows: int, vocab: int):
+        """(pointer, bytes, tensor) of the workspace a call needs: the given one, or one made here."""
+        n = ctypes.c_int64(0)
+        _check(size_call(rows, vocab, ctypes.byref(n)))
+        if given is None:
+            if n.value == 0:
+                return None, 0, None
+            given = self.empty(n.value, self._torch.uint8)
+        if given.device != self.device or not given.is_contiguous():
+            raise ValueError("workspace must be contiguous and on the logits' device")
+        return given.data_ptr(), given.numel() * given.element_size(), given
 
 
 def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None, repetition=None,
@@ -484,21 +496,19 @@ def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None
     logits [n, V]; history [n, L] ids; lengths, repetition, frequency, presence, inv_temperature [n];
     bias, noise [n, V] or [V]; mask [n, (V + 31) // 32] or one row, int32 words; out [rows, V]; choice
     [rows] uint8, int32 or int64.  Row r reads row r % n of each; rows defaults to the logits' n."""
-    import torch
-    n, V = _logits_shape(logits)
+    n, V, dev = _logits_shape(logits)
     rows = n if rows is None else int(rows)
-    dev = logits.device
-    if out is None and choice is None:
-        with torch.cuda.stream(stream):
-            out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
-    args = [_operand(logits, "logits", dev), _operand(history, "history", dev), _operand(lengths, "lengths", dev, True),
-            _operand(repetition, "repetition", dev, True), _operand(frequency, "frequency", dev, True),
-            _operand(presence, "presence", dev, True), _operand(bias, "bias", dev),
-            _operand(inv_temperature, "inv_temperature", dev, True), _operand(mask, "mask", dev),
-            _operand(noise, "noise", dev), _operand(out, "out", dev), _operand(choice, "choice", dev, True)]
-    ws, size, _keep = (None, 0, None) if choice is None else \
-        _workspace(workspace, lib.emo_adjust_workspace, rows, V, dev, stream)
-    _check(_on_device(dev, stream, lambda st: lib.emo_adjust_logits(rows, V, *map(_ref, args), ws, size, st)))
+    with _Place(dev, stream) as at:
+        if out is None and choice is None:
+            out = at.empty((rows, V), logits.dtype)
+        ws, size, _keep = (None, 0, None) if choice is None else at.workspace(workspace, lib.emo_adjust_workspace, rows, V)
+        _check(lib.emo_adjust_logits(
+            rows, V, _operand(logits, "logits", dev), _operand(history, "history", dev),
+            _operand(lengths, "lengths", dev, True), _operand(repetition, "repetition", dev, True),
+            _operand(frequency, "frequency", dev, True), _operand(presence, "presence", dev, True),
+            _operand(bias, "bias", dev), _operand(inv_temperature, "inv_temperature", dev, True),
+            _operand(mask, "mask", dev), _operand(noise, "noise", dev), _operand(out, "out", dev),
+            _operand(choice, "choice", dev, True), ws, size, _stream(None)))
     return out, choice
 
 
@@ -507,17 +517,15 @@ def distill_forward(logits, ids, teacher, temperature: float = 1.0, *, mask=None
     """Cross entropy of the logits [N, V] against a teacher's top entries (emo_distill_forward):
     ids [n, K], teacher [n, K] or one row each.  Returns (loss [N], stats [N, 2] for the backward
     pass), allocated when not given.  Autograd does not see it: distill_backward is the gradient."""
-    import torch
-    N, V = _logits_shape(logits)
-    dev = logits.device
-    with torch.cuda.stream(stream):
-        loss = torch.empty(N, dtype=torch.float32, device=dev) if loss is None else loss
-        stats = torch.empty((N, 2), dtype=torch.float32, device=dev) if stats is None else stats
-    args = [_operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev)]
-    outs = [_operand(mask, "mask", dev), _operand(loss, "loss", dev, True), _operand(stats, "stats", dev)]
-    ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, dev, stream)
-    _check(_on_device(dev, stream, lambda st: lib.emo_distill_forward(
-        N, V, *map(_ref, args), float(temperature), *map(_ref, outs), ws, size, st)))
+    N, V, dev = _logits_shape(logits)
+    with _Place(dev, stream) as at:
+        loss = at.empty(N) if loss is None else loss
+        stats = at.empty((N, 2)) if stats is None else stats
+        ws, size, _keep = at.workspace(workspace, lib.emo_distill_workspace, N, V)
+        _check(lib.emo_distill_forward(
+            N, V, _operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev),
+            float(temperature), _operand(mask, "mask", dev), _operand(loss, "loss", dev, True),
+            _operand(stats, "stats", dev), ws, size, _stream(None)))
     return loss, stats
 
 
@@ -526,17 +534,13 @@ def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, s
     """Gradient [N, V] of sum(scale * loss) by the logits, from the statistics that distill_forward
     returned for the same operands (emo_distill_backward); scale [n] or None (1).  `grad` may be the
     logits."""
-    import torch
-    N, V = _logits_shape(logits)
-    dev = logits.device
-    if grad is None:
-        with torch.cuda.stream(stream):
-            grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
-    args = [_operand(logits, "logits", dev), _operand(stats, "stats", dev), _operand(ids, "ids", dev),
-            _operand(teacher, "teacher", dev)]
-    outs = [_operand(scale, "scale", dev, True), _operand(mask, "mask", dev), _operand(grad, "grad", dev)]
-    _check(_on_device(dev, stream, lambda st: lib.emo_distill_backward(
-        N, V, *map(_ref, args), float(temperature), *map(_ref, outs), st)))
+    N, V, dev = _logits_shape(logits)
+    with _Place(dev, stream) as at:
+        grad = at.empty((N, V), logits.dtype) if grad is None else grad
+        _check(lib.emo_distill_backward(
+            N, V, _operand(logits, "logits", dev), _operand(stats, "stats", dev), _operand(ids, "ids", dev),
+            _operand(teacher, "teacher", dev), float(temperature), _operand(scale, "scale", dev, True),
+            _operand(mask, "mask", dev), _operand(grad, "grad", dev), _stream(None)))
     return grad
 
 
@@ -544,18 +548,15 @@ def distill_step(logits, ids, teacher, temperature: float = 1.0, *, scale=None, 
                  workspace=None, stream=None):
     """Loss [N] and gradient [N, V] in one call (emo_distill_step), for a scale known beforehand (e.g.
     [1 / N]).  `grad` may be the logits."""
-    import torch
-    N, V = _logits_shape(logits)
-    dev = logits.device
-    with torch.cuda.stream(stream):
-        loss = torch.empty(N, dtype=torch.float32, device=dev) if loss is None else loss
-        grad = torch.empty((N, V), dtype=logits.dtype, device=dev) if grad is None else grad
-    args = [_operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev)]
-    outs = [_operand(scale, "scale", dev, True), _operand(mask, "mask", dev), _operand(loss, "loss", dev, True),
-            _operand(grad, "grad", dev)]
-    ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, dev, stream)
-    _check(_on_device(dev, stream, lambda st: lib.emo_distill_step(
-        N, V, *map(_ref, args), float(temperature), *map(_ref, outs), ws, size, st)))
+    N, V, dev = _logits_shape(logits)
+    with _Place(dev, stream) as at:
+        loss = at.empty(N) if loss is None else loss
+        grad = at.empty((N, V), logits.dtype) if grad is None else grad
+        ws, size, _keep = at.workspace(workspace, lib.emo_distill_workspace, N, V)
+        _check(lib.emo_distill_step(
+            N, V, _operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev),
+            float(temperature), _operand(scale, "scale", dev, True), _operand(mask, "mask", dev),
+            _operand(loss, "loss", dev, True), _operand(grad, "grad", dev), ws, size, _stream(None)))
     return loss, grad
 
 
