@@ -35,6 +35,18 @@ __device__ __forceinline__ const T *row_of(const Mat &m, uint32_t r) {
     return reinterpret_cast<const T *>(m.data) + static_cast<int64_t>(row_index(m, r)) * m.row_stride;
 }
 
+// An operand with a row per group of lanes: its row's address is one 32-bit multiplication and addition
+// (the stride in bytes below 2^32), and a kernel holds six scalar registers of it.
+struct Rows {
+    const char *data;
+    uint32_t stride, rows, magic, shift;
+};
+
+__device__ __forceinline__ const char *row_at(const Rows &m, uint32_t r) {
+    if (m.magic) r -= (__umulhi(r, m.magic) >> m.shift) * m.rows;
+    return m.data + static_cast<uint64_t>(r) * m.stride;
+}
+
 __device__ __forceinline__ float row_value(const Mat &m, uint32_t r, float absent) {
     return m.data ? *row_of<float>(m, r) : absent;
 }
@@ -163,11 +175,37 @@ __device__ __forceinline__ void store_chunk(O *row, int64_t v, int32_t V, const 
     }
 }
 
-// The mask's bits of the N entries from v on, a multiple of N (N 4 or 8): a row's words are read by the byte.
+// The mask's bits of the N entries from v on, a multiple of N (N 4 or 8), of a row of V: a row's words are
+// read by the byte.  Entries from V on are not allowed.
 template <int N>
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t *mask, int64_t v) {
-    if (!mask) return (1u << N) - 1;
-    return (reinterpret_cast<const uint8_t *>(mask)[v >> 3] >> (v & 7)) & ((1u << N) - 1);
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t *mask, int64_t v, int32_t V) {
+    const uint32_t all = v + N <= V ? (1u << N) - 1 : (1u << (V - v)) - 1;
+    if (!mask) return all;
+    return (reinterpret_cast<const uint8_t *>(mask)[v >> 3] >> (v & 7)) & all;
+}
+
+// Reductions over groups of 2^lg neighbouring lanes, lg <= 4, to every lane: exchanges within rows of 16
+// lanes are operand modifiers (DPP), where a shuffle goes through LDS.
+template <int Control>
+__device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(x, x, Control, 0xf, 0xf, false); }
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+
+template <typename F>
+__device__ __forceinline__ int group_reduce(int x, int lg, const F &f) {
+    if (lg > 0) x = f(x, dpp<kSwap1>(x));
+    if (lg > 1) x = f(x, dpp<kSwap2>(x));
+    if (lg > 2) x = f(x, dpp<kMirror8>(x));      // the quads are uniform by now: a mirror exchanges them
+    if (lg > 3) x = f(x, dpp<kMirror16>(x));
+    return x;
+}
+__device__ __forceinline__ float group_max(float x, int lg) {
+    return __int_as_float(group_reduce(__float_as_int(x), lg, [](int a, int b) { return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b))); }));
+}
+__device__ __forceinline__ float group_sum(float x, int lg) {
+    return __int_as_float(group_reduce(__float_as_int(x), lg, [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
+__device__ __forceinline__ int group_min(int x, int lg) {
+    return group_reduce(x, lg, [](int a, int b) { return min(a, b); });
 }
 
 __device__ __forceinline__ bool allowed(const uint32_t *mask, int32_t v) {
@@ -195,7 +233,7 @@ emo_status launched(const char *what) {
 
 constexpr int64_t kMaxRows = int64_t(1) << 31;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
-constexpr int64_t kMaxBlocks = int64_t(1) << 20;    // workgroups of a launch: kernels go on by strides
+constexpr int64_t kMaxBlocks = int64_t(1) << 22;    // workgroups of a launch: more go into further launches
 
 constexpr unsigned bit(int dtype) { return 1u << dtype; }
 constexpr unsigned kFloats = bit(EMO_F32) | bit(EMO_F16) | bit(EMO_BF16);
@@ -299,6 +337,14 @@ struct Checker {
     }
 };
 
+// The operand for row_at; false if its stride does not fit.
+bool narrow(const Mat &m, Rows *out) {
+    const int64_t bytes = m.row_stride * size_of(m.dtype);
+    if (m.data && bytes >= (int64_t(1) << 32)) return false;
+    *out = {m.data, static_cast<uint32_t>(bytes), m.rows, m.magic, m.shift};
+    return true;
+}
+
 emo_status check_sizes(int64_t rows, int64_t vocab) {
     if (rows < 0 || rows >= kMaxRows) return fail(EMO_ERR_INVALID_ARGUMENT, "rows %lld outside [0, 2^31)", (long long)rows);
     if (vocab < 1 || vocab >= kMaxRows) return fail(EMO_ERR_INVALID_ARGUMENT, "vocab %lld outside [1, 2^31)", (long long)vocab);
@@ -309,6 +355,13 @@ emo_status check_written(const emo_tensor *out, const emo_tensor *logits, const 
     if (out && out->dtype != logits->dtype && out->dtype != EMO_F32)
         return fail(EMO_ERR_INVALID_ARGUMENT, "%s must have the logits' type or fp32", name);
     return EMO_OK;
+}
+
+// Launches `blocks` workgroups, launch(first block, count) for each kMaxBlocks of them.
+template <typename F>
+void in_launches(int64_t blocks, const F &launch) {
+    for (int64_t b = 0; b < blocks; b += kMaxBlocks)
+        launch(b, static_cast<unsigned>(blocks - b < kMaxBlocks ? blocks - b : kMaxBlocks));
 }
 
 unsigned row_blocks(int64_t rows) { return static_cast<unsigned>(rows < kMaxBlocks ? rows : kMaxBlocks); }

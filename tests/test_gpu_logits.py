@@ -207,6 +207,23 @@ def test_adjust_defaults_and_refusals(torch, emo):
     assert e is None and c.numel() == 0
 
 
+@pytest.mark.parametrize("V", [3, 5, 61, 70, 2051])
+def test_adjust_odd_rates(torch, emo, V):
+    """Rates of any value: a negative, zero or infinite temperature turns no padding behind a row into an entry."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(size=(6, V)).astype(np.float32)
+    x[:, 0] = -np.inf
+    h = rng.integers(0, V, size=(6, 4))
+    kw = {"repetition": np.float32([0, -1, np.inf, np.nan, 1, 2]), "frequency": np.float32([0, -1, np.inf, 1, 0, 0]),
+          "presence": np.float32([0, 1, -1, 0, -np.inf, 0]), "inv_temperature": np.float32([-1, -2, 0, np.inf, -0.5, np.nan])}
+    for mask in (None, orc.mask_words(rng.random((6, V)) < 0.5)):
+        want, wc = orc.adjust(6, x, history=h, mask=mask, **kw)
+        O, C = emo.adjust_logits(dev(torch, x), history=dev(torch, h, "i32"), mask=dev(torch, mask), out=torch.empty((6, V), device="cuda"),
+                                 choice=torch.empty(6, dtype=torch.int32, device="cuda"), **{k: dev(torch, v) for k, v in kw.items()})
+        bits_equal(torch, O, want, "f32", "adjusted")
+        assert C.cpu().tolist() == wc.tolist()
+
+
 def test_adjust_masks_that_leave_little(torch, emo):
     """Nothing, only -inf, only the lowest value, only NaN; a byte choice without an entry is 255."""
     for V in (5, 70, 5000):
