@@ -1,6 +1,8 @@
 // Distillation of logits from a teacher's top entries (emo_distill_forward, _backward, _step).
 #include "emo_logits.h"
 
+#include <algorithm>
+
 namespace {
 
 struct DistillArgs {
@@ -26,116 +28,437 @@ __device__ __forceinline__ float wave_max(float x) {
     return x;
 }
 
-// Sum (or maximum) over the workgroup, to every thread; s_red has a slot per wave.
-template <bool Max>
+// Sum (or maximum) over the workgroup, to every thread, in a fixed order; s_red has a slot per wave.
+template <int Threads, bool Max>
 __device__ __forceinline__ float block_reduce(float x, float *s_red) {
     x = Max ? wave_max(x) : wave_sum(x);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) s_red[threadIdx.x / 64] = x;
-    __syncthreads();
-    x = s_red[0];
-    for (int w = 1; w < kThreads / 64; ++w) x = Max ? fmaxf(x, s_red[w]) : x + s_red[w];
+    if constexpr (Threads > 64) {
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) s_red[threadIdx.x / 64] = x;
+        __syncthreads();
+        x = s_red[0];
+        for (int w = 1; w < Threads / 64; ++w) x = Max ? fmaxf(x, s_red[w]) : x + s_red[w];
+    }
     return x;
 }
 
-// A workgroup per row.  Forward: the greatest logit, then the sum of exponentials below it.  The
-// teacher's probabilities lie in LDS; the gradient goes tile after tile, each tile's probabilities
-// gathered by entry in the list's order, so that equal ids add up in a fixed order.
-template <typename T, typename O, bool Forward, bool Backward>
-__global__ void __launch_bounds__(kThreads) distill_row_kernel(DistillArgs a) {
-    __shared__ int32_t s_id[kMaxEntries];
-    __shared__ float s_p[kMaxEntries];
-    __shared__ float s_red[kThreads / 64];
-    const int tid = threadIdx.x;
-    const int K = a.entries;
-    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const T *logits = row_of<T>(a.logits, r);
-        const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
-        float m = -INFINITY, s = 0.f;
-        if (Forward) {
-            for (int64_t v = tid; v < a.vocab; v += kThreads)
-                if (allowed(mask, static_cast<int32_t>(v))) m = fmaxf(m, static_cast<float>(logits[v]));
-            m = block_reduce<true>(m, s_red);
-            const float ref = m == -INFINITY ? 0.f : m;
-            for (int64_t v = tid; v < a.vocab; v += kThreads)
-                if (allowed(mask, static_cast<int32_t>(v)))
-                    s += exp2f((static_cast<float>(logits[v]) - ref) * a.log2e_tau);
-            s = block_reduce<false>(s, s_red);
-            if (a.stats_out && tid == 0) {
-                float *st = reinterpret_cast<float *>(a.stats_out) + static_cast<int64_t>(r) * a.stats_stride;
-                st[0] = m;
-                st[1] = s;
-            }
-        } else {
-            const float *st = row_of<float>(a.stats, r);
-            m = st[0];
-            s = st[1];
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row's teacher in LDS, K places each: the entry's id (-1: does not count), its probability, the logit at
+// the id, and the probability summed over equal ids.
+struct Teacher {
+    int32_t *id;
+    float *p, *x, *sum;
+};
+constexpr int kTeacherBytes = 16;       // LDS of an entry
+
+__device__ __forceinline__ Teacher teacher_in(float4 *lds, int K) {
+    const int places = (K + 3) / 4 * 4;
+    float *f = reinterpret_cast<float *>(lds);
+    return {reinterpret_cast<int32_t *>(lds), f + places, f + 2 * places, f + 3 * places};
+}
+
+// Loads a row's teacher and makes its probabilities, by one wave (the others stream meanwhile): ids outside
+// [lo, hi) count for the probabilities, but their logits are not read.  True if any entry counts.
+template <typename T>
+__device__ __forceinline__ bool load_teacher(const DistillArgs &a, uint32_t r, const T *logits, const uint32_t *mask, int64_t lo,
+                                             int64_t hi, const Teacher &t) {
+    const int K = a.entries, lane = threadIdx.x % 64;
+    const uint32_t irow = row_index(a.ids, r), trow = row_index(a.teacher, r);
+    float tm = -INFINITY;
+    for (int k = lane; k < K; k += 64) {
+        int32_t id = load_id(a.ids, irow, k, a.vocab);
+        const float v = load_float(a.teacher, trow, k);
+        if (id >= 0 && (v == -INFINITY || !allowed(mask, id))) id = -1;
+        t.id[k] = id;
+        t.p[k] = v;
+        if (id >= lo && id < hi) t.x[k] = static_cast<float>(logits[id]);
+        if (id >= 0) tm = fmaxf(tm, fmaxf(v, -3.4028235e38f));      // a NaN that counts is no -infinity
+    }
+    for (int k = K + lane; k < (K + 3) / 4 * 4; k += 64) t.id[k] = -1;
+    tm = wave_max(tm);
+    float total = 0.f;
+    for (int k = lane; k < K; k += 64) {
+        const float e = t.id[k] >= 0 ? exp2_fast((t.p[k] - tm) * a.log2e_tau) : 0.f;
+        t.p[k] = e;
+        total += e;
+    }
+    total = wave_sum(total);
+    for (int k = lane; k < K; k += 64) t.p[k] = t.p[k] / total;
+    return tm > -INFINITY;
+}
+
+// The probabilities of equal ids in [lo, hi) summed in the list's order: sum[k] at the first entry of an id,
+// -1 at its others.  K comparisons an entry, four a step, by as many threads as there are entries.
+template <int Threads>
+__device__ __forceinline__ void sum_equal_ids(const Teacher &t, int K, int64_t lo, int64_t hi) {
+    for (int k = threadIdx.x; k < K; k += Threads) {
+        const int32_t id = t.id[k];
+        if (id < 0 || id < lo || id >= hi) {
+            t.sum[k] = -1.f;
+            continue;
         }
-        const uint32_t irow = row_index(a.ids, r), trow = row_index(a.teacher, r);
-        float tm = -INFINITY;
-        float any = 0.f;
-        for (int k = tid; k < K; k += kThreads) {
-            int32_t id = load_id(a.ids, irow, k, a.vocab);
-            const float t = load_float(a.teacher, trow, k);
-            if (id >= 0 && (t == -INFINITY || !allowed(mask, id))) id = -1;
-            s_id[k] = id;
-            s_p[k] = t;
-            if (id >= 0) {
-                tm = fmaxf(tm, t);
-                any = 1.f;
-            }
+        float sum = 0.f;
+        bool first = true;
+        for (int i = 0; i < K; i += 4) {
+            const int4 other = *reinterpret_cast<const int4 *>(t.id + i);
+            const float4 p = *reinterpret_cast<const float4 *>(t.p + i);
+            sum += other.x == id ? p.x : 0.f;
+            sum += other.y == id ? p.y : 0.f;
+            sum += other.z == id ? p.z : 0.f;
+            sum += other.w == id ? p.w : 0.f;
+            first = first && !((other.x == id && i < k) || (other.y == id && i + 1 < k) || (other.z == id && i + 2 < k));
+            first = first && !(other.w == id && i + 3 < k);
         }
-        tm = block_reduce<true>(tm, s_red);
-        const bool has = block_reduce<true>(any, s_red) > 0.f;
-        float ts = 0.f;
-        for (int k = tid; k < K; k += kThreads) {
-            s_p[k] = s_id[k] >= 0 ? exp2f((s_p[k] - tm) * a.log2e_tau) : 0.f;
-            ts += s_p[k];
-        }
-        ts = block_reduce<false>(ts, s_red);
-        float loss = 0.f;
-        for (int k = tid; k < K; k += kThreads) {
-            if (s_id[k] < 0) continue;
-            const float p = s_p[k] / ts;
-            s_p[k] = p;
-            if (Forward && p != 0.f) loss += p * (logf(s) - (static_cast<float>(logits[s_id[k]]) - m) * a.inv_tau);
-        }
-        if (Forward && a.loss) {
-            loss = block_reduce<false>(loss, s_red);
-            if (tid == 0)
-                reinterpret_cast<float *>(a.loss)[static_cast<int64_t>(r) * a.loss_stride] = a.tau * a.tau * loss;
-        }
-        if (Backward) {
-            __syncthreads();
-            const float c = row_value(a.scale, r, 1.f) * a.tau;
-            O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride;
-            for (int64_t i = tid; i < a.vocab; i += kThreads) {
-                const int32_t v = static_cast<int32_t>(i);
-                float g = 0.f;
-                if (has && allowed(mask, v)) {
-                    float p = 0.f;
-                    for (int k = 0; k < K; ++k) p += s_id[k] == v ? s_p[k] : 0.f;
-                    g = c * (exp2f((static_cast<float>(logits[v]) - m) * a.log2e_tau) / s - p);
-                }
-                grad[v] = static_cast<O>(g);
-            }
-        }
-        __syncthreads();
+        t.sum[k] = first ? sum : -1.f;
     }
 }
 
-template <bool Forward, bool Backward>
-struct DistillLaunch {
-    const DistillArgs &a;
-    hipStream_t st;
-    template <typename T, typename O>
-    void run() const {
-        hipLaunchKernelGGL((distill_row_kernel<T, O, Forward, Backward>), dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
+// The loss, by one wave: the entries' distances below the row's logarithm of sums.
+__device__ __forceinline__ float teacher_loss(const DistillArgs &a, const Teacher &t, float m, float s) {
+    const float log_s = logf(s);
+    float loss = 0.f;
+    for (int k = threadIdx.x % 64; k < a.entries; k += 64)
+        if (t.id[k] >= 0 && t.p[k] != 0.f) loss += t.p[k] * (log_s - (t.x[k] - m) * a.inv_tau);
+    return wave_sum(loss) * a.tau * a.tau;
+}
+
+__device__ __forceinline__ void store_stats(const DistillArgs &a, uint32_t r, float m, float s) {
+    float *st = reinterpret_cast<float *>(a.stats_out) + static_cast<int64_t>(r) * a.stats_stride;
+    st[0] = m;
+    st[1] = s;
+}
+
+__device__ __forceinline__ void store_loss(const DistillArgs &a, uint32_t r, float loss) {
+    reinterpret_cast<float *>(a.loss)[static_cast<int64_t>(r) * a.loss_stride] = loss;
+}
+
+// The statistics of one thread's entries so far: the greatest and the sum of exponentials below it.
+struct Running {
+    float m = -INFINITY, s = 0.f;
+};
+
+// Where exponents are measured from: the maximum, or 0 if there is none.
+__device__ __forceinline__ float origin(float m) { return m == -INFINITY ? 0.f : m; }
+
+// The compiler forgets what it knows of the chunks: else it keeps every entry as a float from one pass over
+// them to the next, twice the registers of 2-byte types (and spills those of long rows), to save the
+// conversion (a shift).
+template <int C>
+__device__ __forceinline__ void anew(u32x4 (&raw)[C]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) asm volatile("" : "+v"(raw[c]));
+}
+
+// Adds the entries of C chunks and one more: one maximum and one change of origin for all of them.
+template <typename T, int C>
+__device__ __forceinline__ void add_entries(Running &run, u32x4 (&raw)[C], float x, float log2e_tau) {
+    constexpr int N = kChunk<T>;
+    float m = fmaxf(run.m, x);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        for (int j = 0; j < N; ++j) m = fmaxf(m, entry<T>(raw[c], j));
+        __builtin_amdgcn_sched_barrier(0);      // a chunk at a time: see anew
+    }
+    anew(raw);
+    const float o = origin(m);
+    float s = run.s * exp2_fast((run.m - o) * log2e_tau) + exp2_fast((x - o) * log2e_tau);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        for (int j = 0; j < N; ++j) s += exp2_fast((entry<T>(raw[c], j) - o) * log2e_tau);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    anew(raw);
+    asm volatile("" : "+v"(s));     // summed here, not where it is read: the exponents of all entries would live until then
+    run = {m, s};
+}
+
+// The workgroup's statistics, to every thread.
+template <int Threads>
+__device__ __forceinline__ Running block_stats(const Running &run, float log2e_tau, float *s_red) {
+    const float m = block_reduce<Threads, true>(run.m, s_red);
+    const float s = block_reduce<Threads, false>(run.s * exp2_fast((run.m - origin(m)) * log2e_tau), s_red);
+    return {m, s};
+}
+
+// What a workgroup holds of a row: n entries from v0 on, those of whole chunks 16 bytes a lane, the rest (fewer
+// than a chunk) an entry a lane.  Masked entries are -infinity.
+template <typename T, int Threads, int C>
+struct Piece {
+    static constexpr bool Early = C <= 8;       // longer rows have no registers to hold the mask's bytes meanwhile
+    u32x4 raw[C];
+    uint32_t bytes[C];
+    float x;            // this lane's entry of the rest, or -infinity
+
+    __device__ __forceinline__ void load(const T *logits, const uint32_t *mask, int32_t n) {
+        const int32_t whole = n / kChunk<T> * kChunk<T>, e = whole + static_cast<int32_t>(threadIdx.x);
+        load_chunks<T, Threads, C>(logits, whole, raw);
+        x = -INFINITY;
+        if (e < n && allowed(mask, e)) x = static_cast<float>(logits[e]);
+        if (Early && mask) load_mask<T, Threads, C>(mask, whole, bytes);
+    }
+
+    // `n` as in load.
+    __device__ __forceinline__ void apply(const uint32_t *mask, int32_t n) {
+        if (!mask) return;
+        if (!Early) load_mask<T, Threads, C>(mask, n / kChunk<T> * kChunk<T>, bytes);
+#pragma unroll
+        for (int c = 0; c < C; ++c) mask_chunk<T>(raw[c], chunk_bits<T>(bytes[c]));
     }
 };
 
-// Workspace bytes of a call.
-int64_t distill_bytes(int64_t, int64_t) { return 0; }
+// Forward: a workgroup per part of a row (`span` entries, a multiple of what it holds at once).  Bound by
+// memory: the next Threads * 32 entries are loaded while these are added.  A row of one part is finished here,
+// others leave their statistics to finish_kernel.
+template <typename T, int Threads>
+__global__ void __launch_bounds__(Threads) forward_kernel(DistillArgs a, uint32_t first, Pieces pieces, int32_t span, float2 *partial) {
+    constexpr int C = 32 / kChunk<T>, Step = Threads * 32;
+    extern __shared__ float4 lds[];
+    __shared__ float s_red[Threads / 64];
+    const int tid = threadIdx.x;
+    const uint32_t local = piece_row(pieces, blockIdx.x), r = first + local, part = blockIdx.x - local * pieces.parts;
+    const int32_t v0 = static_cast<int32_t>(part) * span;
+    const int32_t n = min(span, a.vocab - v0);
+    const T *row = row_of<T>(a.logits, r);
+    const T *logits = row + v0;
+    const uint32_t *row_mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
+    const uint32_t *mask = row_mask ? row_mask + v0 / 32 : nullptr;
+    Piece<T, Threads, C> now, next;
+    next.load(logits, mask, min(n, Step));
+    const Teacher t = teacher_in(lds, a.entries);
+    bool has = false;
+    if (pieces.parts == 1 && a.loss && tid < 64) has = load_teacher(a, r, row, row_mask, 0, a.vocab, t);
+    Running run;
+    for (int32_t at = 0; at < n; at += Step) {
+        now = next;
+        if (n - at > Step) next.load(logits + at + Step, mask ? mask + (at + Step) / 32 : nullptr, min(n - at - Step, Step));
+        now.apply(mask, min(n - at, Step));
+        add_entries<T, C>(run, now.raw, now.x, a.log2e_tau);
+    }
+    run = block_stats<Threads>(run, a.log2e_tau, s_red);
+    if (pieces.parts > 1) {
+        if (tid == 0) partial[static_cast<int64_t>(r) * pieces.parts + part] = {run.m, run.s};
+        return;
+    }
+    if (a.stats_out && tid == 0) store_stats(a, r, run.m, run.s);
+    if (a.loss && tid < 64) {
+        const float loss = has ? teacher_loss(a, t, run.m, run.s) : 0.f;
+        if (tid == 0) store_loss(a, r, loss);
+    }
+}
+
+// The statistics of a row's parts joined, and its loss: a wave per row.
+template <typename T>
+__global__ void __launch_bounds__(64) finish_kernel(DistillArgs a, int64_t first, int32_t parts, const float2 *partial) {
+    extern __shared__ float4 lds[];
+    const uint32_t r = static_cast<uint32_t>(first + blockIdx.x);
+    const Teacher t = teacher_in(lds, a.entries);
+    const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
+    Running run;
+    for (int32_t i = threadIdx.x; i < parts; i += 64) {
+        const float2 p = partial[static_cast<int64_t>(r) * parts + i];
+        const float m = fmaxf(run.m, p.x), o = origin(m);
+        run = {m, run.s * exp2_fast((run.m - o) * a.log2e_tau) + p.y * exp2_fast((p.x - o) * a.log2e_tau)};
+    }
+    run = block_stats<64>(run, a.log2e_tau, nullptr);
+    if (a.stats_out && threadIdx.x == 0) store_stats(a, r, run.m, run.s);
+    if (a.loss) {
+        const bool has = load_teacher(a, r, row_of<T>(a.logits, r), mask, 0, a.vocab, t);
+        const float loss = has ? teacher_loss(a, t, run.m, run.s) : 0.f;
+        if (threadIdx.x == 0) store_loss(a, r, loss);
+    }
+}
+
+// Writes the gradient of a workgroup's piece (n entries from v0 of the row on), and over it that of the
+// teacher's entries.  rate = scale * temperature.
+template <typename T, typename O, int Threads, int C>
+__device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece<T, Threads, C> &piece, const uint32_t *mask, O *grad,
+                                               int32_t v0, int32_t n, bool has, float m, float s, float rate, const Teacher &t) {
+    constexpr int N = kChunk<T>;
+    const int tid = threadIdx.x;
+    const int32_t whole = n / N * N;
+    // a masked entry's exponential is 0; its product with a share that is no number has to be 0 too
+    const float share = rate / s;
+    const bool odd = mask && !(fabsf(share) < INFINITY);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int32_t e = (c * Threads + tid) * N;
+        if (e < whole) {
+            float g[N];
+            for (int j = 0; j < N; ++j) g[j] = has ? share * exp2_fast((entry<T>(piece.raw[c], j) - m) * a.log2e_tau) : 0.f;
+            if (odd)
+                for (int j = 0; j < N; ++j) g[j] = allowed(mask, e + j) ? g[j] : 0.f;
+            store_chunk(grad, e, g);
+        }
+    }
+    if (whole + tid < n) {
+        const float g = share * exp2_fast((piece.x - m) * a.log2e_tau);
+        grad[whole + tid] = static_cast<O>(has && allowed(mask, whole + tid) ? g : 0.f);
+    }
+    if (!has) return;
+    __syncthreads();        // the entries' own values are in memory before the teacher's go over them
+    for (int k = tid; k < a.entries; k += Threads)
+        if (!(t.sum[k] < 0.f))
+            grad[t.id[k] - v0] = static_cast<O>(rate * (exp2_fast((t.x[k] - m) * a.log2e_tau) / s - t.sum[k]));
+}
+
+// Backward: a workgroup per tile of a row.
+template <typename T, typename O, int Threads>
+__global__ void __launch_bounds__(Threads) backward_kernel(DistillArgs a, uint32_t first, Pieces pieces) {
+    constexpr int C = 32 / kChunk<T>, Tile = Threads * 32;
+    extern __shared__ float4 lds[];
+    __shared__ int s_has;
+    const int tid = threadIdx.x;
+    const uint32_t local = piece_row(pieces, blockIdx.x), r = first + local;
+    const int32_t v0 = static_cast<int32_t>(blockIdx.x - local * pieces.parts) * Tile;
+    const int32_t n = min(Tile, a.vocab - v0);
+    const T *row = row_of<T>(a.logits, r);
+    const uint32_t *row_mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
+    const uint32_t *mask = row_mask ? row_mask + v0 / 32 : nullptr;
+    Piece<T, Threads, C> piece;
+    piece.load(row + v0, mask, n);
+    const Teacher t = teacher_in(lds, a.entries);
+    const int64_t hi = static_cast<int64_t>(v0) + n;
+    if (tid < 64) {
+        const bool has = load_teacher(a, r, row, row_mask, v0, hi, t);
+        if (tid == 0) s_has = has;
+    }
+    const float *st = row_of<float>(a.stats, r);
+    const float m = st[0], s = st[1];
+    const float rate = row_value(a.scale, r, 1.f) * a.tau;
+    piece.apply(mask, n);
+    __syncthreads();
+    sum_equal_ids<Threads>(t, a.entries, v0, hi);
+    O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride + v0;
+    write_gradient(a, piece, mask, grad, v0, n, s_has != 0, m, s, rate, t);
+}
+
+// Loss and gradient of rows that fit a workgroup's registers: read once, written once.
+template <typename T, typename O, int Threads, int PerThread>
+__global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t first) {
+    constexpr int C = PerThread / kChunk<T>;
+    extern __shared__ float4 lds[];
+    __shared__ float s_red[Threads / 64];
+    __shared__ int s_has;
+    const int tid = threadIdx.x;
+    const uint32_t r = static_cast<uint32_t>(first + blockIdx.x);
+    const T *logits = row_of<T>(a.logits, r);
+    const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
+    Piece<T, Threads, C> piece;
+    piece.load(logits, mask, a.vocab);
+    const Teacher t = teacher_in(lds, a.entries);
+    if (tid < 64) {
+        const bool has = load_teacher(a, r, logits, mask, 0, a.vocab, t);
+        if (tid == 0) s_has = has;
+    }
+    const float rate = row_value(a.scale, r, 1.f) * a.tau;
+    piece.apply(mask, a.vocab);
+    Running run;
+    add_entries<T, C>(run, piece.raw, piece.x, a.log2e_tau);
+    __syncthreads();
+    sum_equal_ids<Threads>(t, a.entries, 0, a.vocab);
+    run = block_stats<Threads>(run, a.log2e_tau, s_red);
+    const bool has = s_has != 0;
+    if (a.loss && tid < 64) {
+        const float loss = has ? teacher_loss(a, t, run.m, run.s) : 0.f;
+        if (tid == 0) store_loss(a, r, loss);
+    }
+    O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride;
+    write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t);
+}
+
+// ------------------------------------------------------------------------------ launches
+
+// The parts of a row of the forward pass: of whole 8,192 entries, as many as bring 2,048 workgroups (8 a
+// compute unit) while a row has that many.
+struct Parts {
+    int32_t parts, span;
+};
+
+Parts forward_parts(int64_t rows, int64_t vocab) {
+    if (vocab <= 2048) return {1, 2048};
+    const int64_t most = (vocab + 8191) / 8192;
+    const int64_t want = rows >= 2048 ? 1 : std::min<int64_t>(most, (2048 + rows - 1) / std::max<int64_t>(rows, 1));
+    const int64_t span = std::min<int64_t>((most + want - 1) / want * 8192, INT32_MAX / 8192 * 8192);
+    return {static_cast<int32_t>((vocab + span - 1) / span), static_cast<int32_t>(span)};
+}
+
+// Rows that step_kernel holds: up to 131,072 entries of 2 bytes or 65,536 of 4 (half a compute unit's
+// registers); others go by the forward and the backward kernels.
+int64_t resident(int32_t dtype) { return dtype == EMO_F32 ? 65536 : 131072; }
+
+int64_t partial_bytes(int64_t rows, int64_t vocab) {
+    const Parts p = forward_parts(rows, vocab);
+    return p.parts > 1 ? rows * p.parts * static_cast<int64_t>(sizeof(float2)) : 0;
+}
+
+// Workspace bytes of a call: the statistics of the rows' parts, and those of the rows of a step in two passes.
+int64_t distill_bytes(int64_t rows, int64_t vocab) {
+    return partial_bytes(rows, vocab) + (vocab > resident(EMO_F32) ? rows * static_cast<int64_t>(sizeof(float2)) : 0);
+}
+
+unsigned teacher_lds(const DistillArgs &a) { return static_cast<unsigned>((a.entries + 3) / 4 * 4 * kTeacherBytes); }
+
+struct ForwardLaunch {
+    const DistillArgs &a;
+    float2 *partial;
+    hipStream_t st;
+
+    template <typename T, typename>
+    void run() const {
+        const Parts p = forward_parts(a.rows, a.vocab);
+        in_pieces(a.rows, p.parts, [&](uint32_t first, unsigned count, const Pieces &pieces) {
+            if (a.vocab <= 2048)
+                hipLaunchKernelGGL((forward_kernel<T, 64>), dim3(count), dim3(64), teacher_lds(a), st, a, first, pieces, p.span, partial);
+            else
+                hipLaunchKernelGGL((forward_kernel<T, 256>), dim3(count), dim3(256), teacher_lds(a), st, a, first, pieces, p.span, partial);
+        });
+        if (p.parts > 1)
+            in_launches(a.rows, [&](int64_t first, unsigned count) {
+                hipLaunchKernelGGL((finish_kernel<T>), dim3(count), dim3(64), teacher_lds(a), st, a, first, p.parts, partial);
+            });
+    }
+};
+
+struct BackwardLaunch {
+    const DistillArgs &a;
+    hipStream_t st;
+
+    template <typename T, typename O, int Threads>
+    void tiles() const {
+        const int64_t tiles = (static_cast<int64_t>(a.vocab) + Threads * 32 - 1) / (Threads * 32);
+        in_pieces(a.rows, tiles, [&](uint32_t first, unsigned count, const Pieces &pieces) {
+            hipLaunchKernelGGL((backward_kernel<T, O, Threads>), dim3(count), dim3(Threads), teacher_lds(a), st, a, first, pieces);
+        });
+    }
+
+    template <typename T, typename O>
+    void run() const {
+        if (a.vocab <= 2048) tiles<T, O, 64>();
+        else tiles<T, O, 256>();
+    }
+};
+
+struct StepLaunch {
+    const DistillArgs &a;
+    hipStream_t st;
+
+    template <typename T, typename O, int Threads, int PerThread>
+    void rows() const {
+        in_launches(a.rows, [&](int64_t first, unsigned count) {
+            hipLaunchKernelGGL((step_kernel<T, O, Threads, PerThread>), dim3(count), dim3(Threads), teacher_lds(a), st, a, first);
+        });
+    }
+
+    template <typename T, typename O>
+    void run() const {
+        if (a.vocab <= 2048) rows<T, O, 64, 32>();
+        else if (a.vocab <= 8192) rows<T, O, 256, 32>();
+        else if (a.vocab <= 32768) rows<T, O, 512, 64>();
+        else if (a.vocab <= 65536) rows<T, O, 1024, 64>();
+        else if constexpr (sizeof(T) == 2) rows<T, O, 1024, 128>();
+    }
+};
 
 // The operands every distillation call has.
 emo_status distill_operands(Checker &c, DistillArgs &a, int64_t rows, int64_t vocab, const emo_tensor *logits,
@@ -188,7 +511,7 @@ emo_status emo_distill_forward(int64_t rows, int64_t vocab, const emo_tensor *lo
     a.loss_stride = l.row_stride;
     a.stats_out = const_cast<char *>(st.data);
     a.stats_stride = st.row_stride;
-    by_types(a.logits.dtype, EMO_F32, DistillLaunch<true, false>{a, static_cast<hipStream_t>(stream)});
+    by_types(a.logits.dtype, EMO_F32, ForwardLaunch{a, static_cast<float2 *>(workspace), static_cast<hipStream_t>(stream)});
     return launched("emo_distill_forward");
 }
 
@@ -211,7 +534,7 @@ emo_status emo_distill_backward(int64_t rows, int64_t vocab, const emo_tensor *l
     if (rows == 0) return emo::report(EMO_OK, "");
     a.grad = const_cast<char *>(g.data);
     a.grad_stride = g.row_stride;
-    by_types(a.logits.dtype, g.dtype, DistillLaunch<false, true>{a, static_cast<hipStream_t>(stream)});
+    by_types(a.logits.dtype, g.dtype, BackwardLaunch{a, static_cast<hipStream_t>(stream)});
     return launched("emo_distill_backward");
 }
 
@@ -236,7 +559,22 @@ emo_status emo_distill_step(int64_t rows, int64_t vocab, const emo_tensor *logit
     a.loss_stride = l.row_stride;
     a.grad = const_cast<char *>(g.data);
     a.grad_stride = g.row_stride;
-    by_types(a.logits.dtype, g.dtype, DistillLaunch<true, true>{a, static_cast<hipStream_t>(stream)});
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (vocab <= resident(a.logits.dtype)) {
+        by_types(a.logits.dtype, g.dtype, StepLaunch{a, st});
+        return launched("emo_distill_step");
+    }
+    // the rows' statistics behind those of their parts
+    char *kept = static_cast<char *>(workspace) + partial_bytes(rows, vocab);
+    a.stats_out = kept;
+    a.stats_stride = 2;
+    by_types(a.logits.dtype, EMO_F32, ForwardLaunch{a, static_cast<float2 *>(workspace), st});
+    a.stats = {};
+    a.stats.data = kept;
+    a.stats.row_stride = 2;
+    a.stats.rows = a.rows;
+    a.stats.dtype = EMO_F32;
+    by_types(a.logits.dtype, g.dtype, BackwardLaunch{a, st});
     return launched("emo_distill_step");
 }
 

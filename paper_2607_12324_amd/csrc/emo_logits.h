@@ -6,6 +6,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <type_traits>
+
 #include "emo_internal.h"
 
 namespace {
@@ -46,6 +48,15 @@ __device__ __forceinline__ const char *row_at(const Rows &m, uint32_t r) {
     if (m.magic) r -= (__umulhi(r, m.magic) >> m.shift) * m.rows;
     return m.data + static_cast<uint64_t>(r) * m.stride;
 }
+
+// The workgroups of rows of `parts` pieces: workgroup b < 2^31 of a launch takes piece b % parts of the
+// launch's row b / parts (divided as in row_index: the compiler's 64-bit division is 100 scalar
+// instructions a workgroup).
+struct Pieces {
+    uint32_t parts, magic, shift;
+};
+
+__device__ __forceinline__ uint32_t piece_row(const Pieces &p, uint32_t b) { return p.magic ? __umulhi(b, p.magic) >> p.shift : b; }
 
 __device__ __forceinline__ float row_value(const Mat &m, uint32_t r, float absent) {
     return m.data ? *row_of<float>(m, r) : absent;
@@ -95,31 +106,68 @@ __device__ __forceinline__ uint32_t bits_of(float x) {
     else return __builtin_bit_cast(uint16_t, static_cast<T>(x));
 }
 
-// The chunk at entry v of a row of V; entries from V on are -infinity.
+// Two floats as two 16-bit values of a word, each rounded to nearest even.
 template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const T *row, int64_t v, int32_t V) {
-    constexpr int N = kChunk<T>;
-    if (v + N <= V) return *reinterpret_cast<const u32x4_any *>(row + v);
-    const uint32_t none = bits_of<T>(-INFINITY);
-    u32x4 raw;
-    for (int w = 0; w < 4; ++w) {
-        if constexpr (N == 4) {
-            raw[w] = v + w < V ? reinterpret_cast<const uint32_t *>(row)[v + w] : none;
-        } else {
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(row);
-            const uint32_t lo = v + 2 * w < V ? p[v + 2 * w] : none;
-            const uint32_t hi = v + 2 * w + 1 < V ? p[v + 2 * w + 1] : none;
-            raw[w] = lo | hi << 16;
-        }
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), t2));
+}
+
+// Entry v of a row, or of a tile of a wide one, below 2^30: addressed as a scalar base and 32 bits of bytes.
+template <typename P>
+__device__ __forceinline__ P *at_entry(P *row, int32_t v) {
+    using B = typename std::conditional<std::is_const<P>::value, const char, char>::type;
+    return reinterpret_cast<P *>(reinterpret_cast<B *>(row) + static_cast<uint32_t>(v) * static_cast<uint32_t>(sizeof(P)));
+}
+
+// The whole chunk at entry v of a row.
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T *row, int32_t v) {
+    return *reinterpret_cast<const u32x4_any *>(at_entry(row, v));
+}
+
+// The chunks of a workgroup's thread among `whole` entries (a multiple of the chunk): chunk c is at entry
+// (c * Threads + thread) * kChunk; those behind are -infinity.  No load waits for another: what a row has
+// beyond whole chunks is taken by a lane an entry, apart from this (a guard per entry here costs a wait
+// per chunk and, where a row fills the registers, spills).
+template <typename T, int Threads, int C>
+__device__ __forceinline__ void load_chunks(const T *row, int32_t whole, u32x4 (&raw)[C]) {
+    const uint32_t none = sizeof(T) == 4 ? 0xff800000u : bits_of<T>(-INFINITY) * 0x10001u;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int32_t e = (c * Threads + static_cast<int32_t>(threadIdx.x)) * kChunk<T>;
+        raw[c] = u32x4{none, none, none, none};
+        if (e < whole) raw[c] = load_chunk(row, e);
     }
-    return raw;
+}
+
+// The mask's bits of those chunks, a byte each: chunk_bits takes the chunk's own.
+template <typename T, int Threads, int C>
+__device__ __forceinline__ void load_mask(const uint32_t *mask, int32_t whole, uint32_t (&bytes)[C]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int32_t e = (c * Threads + static_cast<int32_t>(threadIdx.x)) * kChunk<T>;
+        bytes[c] = 0xff;
+        if (e < whole) bytes[c] = reinterpret_cast<const uint8_t *>(mask)[static_cast<uint32_t>(e) >> 3];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t chunk_bits(uint32_t byte) {
+    return kChunk<T> == 8 ? byte : byte >> (threadIdx.x & 1) * 4 & 0xfu;
 }
 
 // Four entries at v of a row of V, as floats (-infinity from V on).
 template <typename T>
 __device__ __forceinline__ void load_four(const T *row, int32_t v, int32_t V, float (&x)[4]) {
     if constexpr (sizeof(T) == 4) {
-        const u32x4 raw = load_chunk(row, v, V);
+        u32x4 raw;
+        if (v + 4 <= V) {
+            raw = load_chunk(row, v);
+        } else {
+            for (int w = 0; w < 4; ++w) raw[w] = v + w < V ? reinterpret_cast<const uint32_t *>(row)[v + w] : 0xff800000u;
+        }
         for (int j = 0; j < 4; ++j) x[j] = entry<T>(raw, j);
     } else {
         u32x4 raw = {0, 0, 0, 0};
@@ -137,38 +185,50 @@ __device__ __forceinline__ void load_four(const T *row, int32_t v, int32_t V, fl
     }
 }
 
+// The floats of a whole chunk.
+template <int N>
+__device__ __forceinline__ void load_floats(const float *row, int32_t v, float (&f)[N]) {
+    for (int i = 0; i < N; i += 4) {
+        const u32x4 raw = *reinterpret_cast<const u32x4_any *>(at_entry(row, v) + i);
+        for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(raw[j]);
+    }
+}
+
 // N floats at entry v of a row of V (zeros from V on).
 template <int N>
-__device__ __forceinline__ void load_floats(const float *row, int64_t v, int32_t V, float (&f)[N]) {
+__device__ __forceinline__ void load_floats(const float *row, int32_t v, int32_t V, float (&f)[N]) {
     if (v + N <= V) {
-        for (int i = 0; i < N; i += 4) {
-            const u32x4 raw = *reinterpret_cast<const u32x4_any *>(row + v + i);
-            for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(raw[j]);
-        }
+        load_floats(row, v, f);
     } else {
         for (int j = 0; j < N; ++j) f[j] = v + j < V ? row[v + j] : 0.f;
     }
 }
 
-// N values at entry v of a row of V, each rounded once to the row's type.
+// A whole chunk of N values at entry v, each rounded once to the row's type.
 template <typename O, int N>
-__device__ __forceinline__ void store_chunk(O *row, int64_t v, int32_t V, const float (&f)[N]) {
-    if (v + N <= V) {
-        if constexpr (sizeof(O) == 4) {
-            for (int i = 0; i < N; i += 4) {
-                u32x4 raw;
-                for (int j = 0; j < 4; ++j) raw[j] = __float_as_uint(f[i + j]);
-                *reinterpret_cast<u32x4_any *>(row + v + i) = raw;
-            }
-        } else if constexpr (N == 4) {
-            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-            const u32x2 raw = {bits_of<O>(f[0]) | bits_of<O>(f[1]) << 16, bits_of<O>(f[2]) | bits_of<O>(f[3]) << 16};
-            *reinterpret_cast<u32x2_any *>(row + v) = raw;
-        } else {
+__device__ __forceinline__ void store_chunk(O *row, int32_t v, const float (&f)[N]) {
+    if constexpr (sizeof(O) == 4) {
+        for (int i = 0; i < N; i += 4) {
             u32x4 raw;
-            for (int w = 0; w < 4; ++w) raw[w] = bits_of<O>(f[2 * w]) | bits_of<O>(f[2 * w + 1]) << 16;
-            *reinterpret_cast<u32x4_any *>(row + v) = raw;
+            for (int j = 0; j < 4; ++j) raw[j] = __float_as_uint(f[i + j]);
+            *reinterpret_cast<u32x4_any *>(at_entry(row, v) + i) = raw;
         }
+    } else if constexpr (N == 4) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 raw = {pack_two<O>(f[0], f[1]), pack_two<O>(f[2], f[3])};
+        *reinterpret_cast<u32x2_any *>(at_entry(row, v)) = raw;
+    } else {
+        u32x4 raw;
+        for (int w = 0; w < 4; ++w) raw[w] = pack_two<O>(f[2 * w], f[2 * w + 1]);
+        *reinterpret_cast<u32x4_any *>(at_entry(row, v)) = raw;
+    }
+}
+
+// N values at entry v of a row of V.
+template <typename O, int N>
+__device__ __forceinline__ void store_chunk(O *row, int32_t v, int32_t V, const float (&f)[N]) {
+    if (v + N <= V) {
+        store_chunk(row, v, f);
     } else {
         for (int j = 0; j < N; ++j)
             if (v + j < V) row[v + j] = static_cast<O>(f[j]);
@@ -178,10 +238,23 @@ __device__ __forceinline__ void store_chunk(O *row, int64_t v, int32_t V, const 
 // The mask's bits of the N entries from v on, a multiple of N (N 4 or 8), of a row of V: a row's words are
 // read by the byte.  Entries from V on are not allowed.
 template <int N>
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t *mask, int64_t v, int32_t V) {
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t *mask, int32_t v, int32_t V) {
     const uint32_t all = v + N <= V ? (1u << N) - 1 : (1u << (V - v)) - 1;
     if (!mask) return all;
-    return (reinterpret_cast<const uint8_t *>(mask)[v >> 3] >> (v & 7)) & all;
+    return (reinterpret_cast<const uint8_t *>(mask)[static_cast<uint32_t>(v) >> 3] >> (v & 7)) & all;
+}
+
+// Puts -infinity where a chunk's bit is 0.
+template <typename T>
+__device__ __forceinline__ void mask_chunk(u32x4 &raw, uint32_t bits) {
+    constexpr int N = kChunk<T>;
+    if (bits == (1u << N) - 1) return;
+    const auto ones = [&](int j) { return static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - j)) >> 31); };
+    const uint32_t none = sizeof(T) == 4 ? 0xff800000u : bits_of<T>(-INFINITY) * 0x10001u;
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t on = N == 4 ? ones(w) : (ones(2 * w) & 0xffffu) | (ones(2 * w + 1) << 16);
+        raw[w] = (raw[w] & on) | (none & ~on);
+    }
 }
 
 // Reductions over groups of 2^lg neighbouring lanes, lg <= 4, to every lane: exchanges within rows of 16
@@ -233,7 +306,7 @@ emo_status launched(const char *what) {
 
 constexpr int64_t kMaxRows = int64_t(1) << 31;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
-constexpr int64_t kMaxBlocks = int64_t(1) << 22;    // workgroups of a launch: more go into further launches
+constexpr int64_t kMaxBlocks = int64_t(1) << 21;    // workgroups of a launch (below 2^32 threads): more go into further launches
 
 constexpr unsigned bit(int dtype) { return 1u << dtype; }
 constexpr unsigned kFloats = bit(EMO_F32) | bit(EMO_F16) | bit(EMO_BF16);
@@ -246,6 +319,14 @@ int64_t size_of(int32_t dtype) {
         case EMO_I64: return 8;
         default: return 4;
     }
+}
+
+// For 2 <= n < 2^31 and s the least with n <= 2^s: r * (2^(31 + s) / n + 1) >> (31 + s) is r / n for r < 2^31.
+void magic_of(int64_t n, uint32_t *magic, uint32_t *shift) {
+    int s = 1;
+    while ((int64_t(1) << s) < n) ++s;
+    *magic = static_cast<uint32_t>((static_cast<unsigned __int128>(1) << (31 + s)) / static_cast<uint64_t>(n) + 1);
+    *shift = static_cast<uint32_t>(s - 1);
 }
 
 // Checks the operands of one call against its sizes, and their memory against each other.
@@ -293,11 +374,7 @@ struct Checker {
         if (t->rows == 1) {
             m.row_stride = 0;
         } else if (t->rows != rows) {
-            // 2 <= n < 2^31, s = the least with n <= 2^s: r * (2^(31 + s) / n + 1) >> (31 + s) is r / n for r < 2^31
-            int bits = 1;
-            while ((int64_t(1) << bits) < t->rows) ++bits;
-            m.magic = static_cast<uint32_t>((static_cast<unsigned __int128>(1) << (31 + bits)) / static_cast<uint64_t>(t->rows) + 1);
-            m.shift = static_cast<uint32_t>(bits - 1);
+            magic_of(t->rows, &m.magic, &m.shift);
         }
         if (t->cols == 0) return m;
         if (!t->data) return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s has no data", name)), m;
@@ -364,7 +441,17 @@ void in_launches(int64_t blocks, const F &launch) {
         launch(b, static_cast<unsigned>(blocks - b < kMaxBlocks ? blocks - b : kMaxBlocks));
 }
 
-unsigned row_blocks(int64_t rows) { return static_cast<unsigned>(rows < kMaxBlocks ? rows : kMaxBlocks); }
+// Launches the workgroups of rows of `parts` pieces, launch(first row, count, pieces) for as many rows as fit.
+template <typename F>
+void in_pieces(int64_t rows, int64_t parts, const F &launch) {
+    Pieces p = {static_cast<uint32_t>(parts), 0, 0};
+    if (parts > 1) magic_of(parts, &p.magic, &p.shift);
+    const int64_t most = parts < kMaxBlocks ? kMaxBlocks / parts : 1;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = rows - r < most ? rows - r : most;
+        launch(static_cast<uint32_t>(r), static_cast<unsigned>(n * parts), p);
+    }
+}
 
 // Calls f.template run<T, O>() for the logits' type T and the written type O (T or float).
 template <typename F>

@@ -1,8 +1,6 @@
 // Logits adjusted and chosen from (emo_adjust_logits).
 #include "emo_logits.h"
 
-#include <type_traits>
-
 // the values are defined to the bit: no multiplication is fused into an addition
 #pragma clang fp contract(off)
 
@@ -73,22 +71,22 @@ __device__ __forceinline__ RowRates rates_of(const AdjustArgs &a, uint32_t r) {
             row_value(a.inv_temperature, r, 1.f)};
 }
 
-// The penalties on N entries that the history holds n times.
-template <int N>
-__device__ __forceinline__ void penalise(const AdjustArgs &a, const RowRates &rate, float (&x)[N], const uint32_t (&n)[N]) {
-    for (int j = 0; j < N; ++j) {
-        float p = x[j];
-        if (a.repetition.data) p = p > 0.f ? p / rate.repetition : p * rate.repetition;
-        if (a.frequency.data) p = p - static_cast<float>(n[j]) * rate.frequency;
-        if (a.presence.data) p = p - rate.presence;
-        x[j] = n[j] ? p : x[j];
-    }
+// The penalties on an entry that the history holds n > 0 times.
+__device__ __forceinline__ float penalise(const AdjustArgs &a, const RowRates &rate, float x, uint32_t n) {
+    if (a.repetition.data) x = x > 0.f ? x / rate.repetition : x * rate.repetition;
+    if (a.frequency.data) x = x - static_cast<float>(n) * rate.frequency;
+    if (a.presence.data) x = x - rate.presence;
+    return x;
 }
 
+// -infinity where the bit is 0: the bit as a word of ones or zeros selects between the two bit by bit.
 template <int N>
 __device__ __forceinline__ void mask_entries(float (&x)[N], uint32_t bits) {
     if (bits != (1u << N) - 1)
-        for (int j = 0; j < N; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
+        for (int j = 0; j < N; ++j) {
+            const uint32_t on = static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - j)) >> 31);
+            x[j] = __uint_as_float((__float_as_uint(x[j]) & on) | (0xff800000u & ~on));
+        }
 }
 
 __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r) {
@@ -97,92 +95,105 @@ __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r)
     return a.lengths.data ? min(max(*row_of<int32_t>(a.lengths, r), 0), L) : L;
 }
 
-constexpr int kPerThread = 32;      // entries a thread holds
+constexpr uint32_t kUnseen = 0xffffffffu;
 
 // A workgroup per tile of Threads * 32 entries of a row.  Bound by memory: a thread's logits (64 or 128
-// bytes) are all in flight before anything else; while they come, the history's ids in the tile are
-// counted in LDS (Count: 16 bits an entry while the history has fewer ids than that holds, which lets 8
-// workgroups of 256 threads onto a compute unit; integer atomics: any order gives the same counts).  The
-// choice of a row of several tiles goes through `parts`, one best entry a tile, and choose_kernel.
-template <typename T, typename O, int Threads, typename Count>
-__global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, int64_t first, int32_t tiles, Best *parts) {
-    constexpr bool History = !std::is_void<Count>::value;
-    constexpr int N = kChunk<T>, C = kPerThread / N, Tile = Threads * kPerThread;
-    constexpr int PerWord = !History ? 1 : 4 / sizeof(typename std::conditional<History, Count, int>::type);
-    __shared__ alignas(16) uint32_t s_count[History ? Tile / PerWord : 4];
+// bytes) are all in flight before anything else.  While they come, the history's ids in the tile are
+// counted in a table in LDS (a word an entry, kUnseen plus the count; integer atomics: any order gives the
+// same counts), and whoever counts an id first puts the penalised logit in the count's place afterwards:
+// penalties cost a few of the history's ids, not every entry (a division each where any lane of a wave
+// has a seen entry, which is nearly always, took 320 of 700 instructions a chunk).  The choice of a row of
+// several tiles goes through `parts`, one best entry a tile, and choose_kernel.
+template <typename T, typename O, int Threads, int PerThread, bool History>
+__global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint32_t first, Pieces pieces, Best *parts) {
+    constexpr int N = kChunk<T>, C = PerThread / N, Tile = Threads * PerThread;
+    __shared__ alignas(16) uint32_t s_seen[History ? Tile : 4];
     const int tid = threadIdx.x;
-    const int64_t b = first + blockIdx.x;
-    const uint32_t r = static_cast<uint32_t>(tiles == 1 ? b : b / tiles);
-    const int64_t v0 = (b - static_cast<int64_t>(r) * tiles) * Tile;
-    const T *logits = row_of<T>(a.logits, r);
+    const uint32_t local = piece_row(pieces, blockIdx.x), r = first + local, part = blockIdx.x - local * pieces.parts;
+    const int32_t v0 = static_cast<int32_t>(part) * Tile;
+    const int32_t n = min(Tile, a.vocab - v0);      // entries of this tile
+    const int32_t whole = n / N * N, rest = whole + tid;
+    const T *logits = row_of<T>(a.logits, r) + v0;
     u32x4 raw[C];
-    uint32_t bits[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int64_t v = v0 + (c * Threads + tid) * N;
-        if (v < a.vocab) raw[c] = load_chunk(logits, v, a.vocab);
-    }
+    uint32_t bytes[C];
+    load_chunks<T, Threads, C>(logits, whole, raw);
+    float x_rest = rest < n ? static_cast<float>(logits[rest]) : 0.f;
+    const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) + v0 / 32 : nullptr;
+    if (mask) load_mask<T, Threads, C>(mask, whole, bytes);
     const int32_t L = History ? live_history(a, r) : 0;
-    const RowRates rate = rates_of(a, r);
-    const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int64_t v = v0 + (c * Threads + tid) * N;
-        if (v < a.vocab) bits[c] = mask_bits<N>(mask, v, a.vocab);
-    }
+    const float inv_t = row_value(a.inv_temperature, r, 1.f);
     if (History && L > 0) {
         const uint32_t hrow = row_index(a.history, r);
+        const RowRates rate = rates_of(a, r);
 #pragma unroll
-        for (int i = 0; i < Tile / PerWord; i += 4 * Threads) *reinterpret_cast<u32x4 *>(&s_count[i + 4 * tid]) = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < Tile; i += 4 * Threads)
+            *reinterpret_cast<u32x4 *>(&s_seen[i + 4 * tid]) = u32x4{kUnseen, kUnseen, kUnseen, kUnseen};
         __syncthreads();
-        for (int32_t i = tid; i < L; i += Threads) {
-            const int64_t id = load_id(a.history, hrow, i, a.vocab) - v0;
-            if (id >= 0 && id < Tile) atomicAdd(&s_count[id / PerWord], 1u << id % PerWord * 16);
+        uint64_t mine = 0;      // which of this thread's ids it counted first
+        int k = 0;
+        for (int32_t i = tid; i < L; i += Threads, ++k) {
+            const int32_t id = load_id(a.history, hrow, i, a.vocab) - v0;
+            if (id >= 0 && id < n && atomicAdd(&s_seen[id], 1u) == kUnseen && k < 64) mine |= uint64_t(1) << k;
+        }
+        __syncthreads();
+        if (L <= 64 * Threads) {
+            for (; mine; mine &= mine - 1) {
+                const int32_t id = load_id(a.history, hrow, tid + __builtin_ctzll(mine) * Threads, a.vocab) - v0;
+                s_seen[id] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[id]), s_seen[id] + 1));
+            }
+        } else {
+            for (int e = tid; e < n; e += Threads)
+                if (s_seen[e] != kUnseen)
+                    s_seen[e] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
         }
         __syncthreads();
     }
-    const float *bias = a.bias.data ? row_of<float>(a.bias, r) : nullptr;
-    const float *noise = a.noise.data ? row_of<float>(a.noise, r) : nullptr;
-    O *out = reinterpret_cast<O *>(a.out) + static_cast<int64_t>(r) * a.out_stride;
+    const float *bias = a.bias.data ? row_of<float>(a.bias, r) + v0 : nullptr;
+    const float *noise = a.noise.data && a.choice ? row_of<float>(a.noise, r) + v0 : nullptr;
+    O *out = reinterpret_cast<O *>(a.out) + static_cast<int64_t>(r) * a.out_stride + v0;
     Best best = {-INFINITY, INT32_MAX};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int e = (c * Threads + tid) * N;
-        const int64_t v = v0 + e;
-        if (v < a.vocab) {
-            float x[N], f[N];
+        if (e < whole) {
+            float x[N], f[N], g[N];
+            if (bias) load_floats(bias, e, f);
+            if (noise) load_floats(noise, e, g);
             for (int j = 0; j < N; ++j) x[j] = entry<T>(raw[c], j);
             if (History && L > 0) {
-                uint32_t n[N], any = 0;
                 for (int j = 0; j < N; ++j) {
-                    n[j] = PerWord == 1 ? s_count[e + j] : s_count[(e + j) / 2] >> j % 2 * 16 & 0xffffu;
-                    any |= n[j];
+                    const uint32_t seen = s_seen[e + j];
+                    x[j] = seen != kUnseen ? __uint_as_float(seen) : x[j];
                 }
-                if (any) penalise(a, rate, x, n);
             }
-            if (bias) {
-                load_floats(bias, v, a.vocab, f);
+            if (bias)
                 for (int j = 0; j < N; ++j) x[j] = x[j] + f[j];
-            }
             if (a.inv_temperature.data)
-                for (int j = 0; j < N; ++j) x[j] = x[j] * rate.inv_temperature;
-            mask_entries(x, bits[c]);
-            if (a.out) store_chunk(out, v, a.vocab, x);
-            if (a.choice) {
-                if (noise) {
-                    load_floats(noise, v, a.vocab, f);
-                    for (int j = 0; j < N; ++j) x[j] = x[j] + f[j];
-                }
+                for (int j = 0; j < N; ++j) x[j] = x[j] * inv_t;
+            if (mask) mask_entries(x, chunk_bits<T>(bytes[c]));
+            if (a.out) store_chunk(out, e, x);
+            if (noise)
+                for (int j = 0; j < N; ++j) x[j] = x[j] + g[j];
+            if (a.choice)
                 for (int j = 0; j < N; ++j)
-                    if (x[j] > best.value) best = {x[j], static_cast<int32_t>(v) + j};
-            }
+                    if (x[j] > best.value) best = {x[j], e + j};
         }
+    }
+    if (rest < n) {
+        if (History && L > 0 && s_seen[rest] != kUnseen) x_rest = __uint_as_float(s_seen[rest]);
+        if (bias) x_rest = x_rest + bias[rest];
+        if (a.inv_temperature.data) x_rest = x_rest * inv_t;
+        if (!allowed(mask, rest)) x_rest = -INFINITY;
+        if (a.out) out[rest] = static_cast<O>(x_rest);
+        if (noise) x_rest = x_rest + noise[rest];
+        if (x_rest > best.value) best = {x_rest, rest};
     }
     if (a.choice) {
         best = block_best<Threads>(best);
         if (tid == 0) {
-            if (tiles == 1) store_choice(a, r, best);
-            else parts[b] = best;
+            if (best.at != INT32_MAX) best.at += v0;
+            if (pieces.parts == 1) store_choice(a, r, best);
+            else parts[static_cast<int64_t>(r) * pieces.parts + part] = best;
         }
     }
 }
@@ -231,7 +242,8 @@ __global__ void __launch_bounds__(kThreads) adjust_group_kernel(GroupArgs g, int
                     const int32_t id = load_id(a.history, hrow, i, g.vocab) - v;
                     for (int j = 0; j < 4; ++j) n[j] += id == j;
                 }
-                penalise(a, rates_of(a, r[u]), x[u], n);
+                const RowRates rate = rates_of(a, r[u]);
+                for (int j = 0; j < 4; ++j) x[u][j] = n[j] ? penalise(a, rate, x[u][j], n[j]) : x[u][j];
             }
         }
         if (g.bias.data) {
@@ -323,7 +335,7 @@ struct Tiling {
 
 Tiling tiling(int64_t rows, int64_t vocab) {
     const int64_t wide = (vocab + 8191) / 8192;
-    if (vocab > 2048 && rows * wide >= 1024) return {256, wide};
+    if (vocab > 2048 && rows * wide >= 1024) return {512, wide};
     return {64, (vocab + 2047) / 2048};
 }
 
@@ -332,15 +344,13 @@ struct AdjustLaunch {
     Best *parts;
     hipStream_t st;
 
-    template <typename T, typename O, int Threads>
+    template <typename T, typename O, int Threads, int PerThread>
     void tiles(int32_t n) const {
-        in_launches(static_cast<int64_t>(a.rows) * n, [&](int64_t first, unsigned count) {
-            if (!a.history.data)
-                hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, void>), dim3(count), dim3(Threads), 0, st, a, first, n, parts);
-            else if (a.history.cols < 65536)
-                hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, uint16_t>), dim3(count), dim3(Threads), 0, st, a, first, n, parts);
+        in_pieces(a.rows, n, [&](uint32_t first, unsigned count, const Pieces &pieces) {
+            if (a.history.data)
+                hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, PerThread, true>), dim3(count), dim3(Threads), 0, st, a, first, pieces, parts);
             else
-                hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, uint32_t>), dim3(count), dim3(Threads), 0, st, a, first, n, parts);
+                hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, PerThread, false>), dim3(count), dim3(Threads), 0, st, a, first, pieces, parts);
         });
         if (a.choice && n > 1)
             in_launches(a.rows, [&](int64_t first, unsigned count) {
@@ -362,8 +372,8 @@ struct AdjustLaunch {
             return;
         }
         const Tiling t = tiling(a.rows, a.vocab);
-        if (t.threads == 64) tiles<T, O, 64>(static_cast<int32_t>(t.tiles));
-        else tiles<T, O, 256>(static_cast<int32_t>(t.tiles));
+        if (t.threads == 64) tiles<T, O, 64, 32>(static_cast<int32_t>(t.tiles));
+        else tiles<T, O, 512, 16>(static_cast<int32_t>(t.tiles));
     }
 };
 
