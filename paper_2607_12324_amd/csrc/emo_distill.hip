@@ -367,6 +367,160 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t);
 }
 
+// Rows of at most 64 entries: 64 rows a workgroup, in two phases.  The teacher's: a lane per row and a wave per
+// slice of the list, so that level bytes [K][rows] come 64 to a load; each lane adds its slice's weights to
+// its row's table in LDS, entry by entry in the list's order (no two lanes share a table: a fixed order
+// without comparing ids, K adds where K^2 comparisons bounded the call).  The student's: a group of 2^lg
+// lanes per row, four entries a lane.
+struct SmallArgs {
+    int32_t lg, vocab, entries;
+    uint32_t rows;
+    float inv_tau, tau, log2e_tau;
+    Rows logits, ids, teacher, mask, scale, stats;
+    uint32_t id_step, teacher_step;     // bytes from one entry to the next
+    int32_t id_type, teacher_type;
+    char *loss, *stats_out, *grad;
+    uint32_t loss_stride, stats_stride, grad_stride;    // bytes
+};
+
+constexpr int kSmallRows = 64;
+
+__device__ __forceinline__ int32_t small_id(const char *p, int32_t type, int32_t vocab) {
+    int64_t id;
+    if (type == EMO_U8) id = *reinterpret_cast<const uint8_t *>(p);
+    else if (type == EMO_I32) id = *reinterpret_cast<const int32_t *>(p);
+    else id = *reinterpret_cast<const int64_t *>(p);
+    return id >= 0 && id < vocab ? static_cast<int32_t>(id) : -1;
+}
+
+__device__ __forceinline__ float small_float(const char *p, int32_t type) {
+    if (type == EMO_F32) return *reinterpret_cast<const float *>(p);
+    if (type == EMO_F16) return static_cast<float>(*reinterpret_cast<const _Float16 *>(p));
+    return static_cast<float>(*reinterpret_cast<const __bf16 *>(p));
+}
+
+template <typename T, typename O, int Slices, int Most, bool Forward, bool Backward>
+__global__ void __launch_bounds__(kThreads) small_kernel(SmallArgs a, int64_t first) {
+    constexpr int Width = Most + 1, Batch = 16;     // a table's rows start in different banks
+    __shared__ float s_table[Slices][kSmallRows * Width];
+    __shared__ float s_max[Slices][kSmallRows], s_sum[Slices][kSmallRows];
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const uint32_t r0 = static_cast<uint32_t>((first + blockIdx.x) * kSmallRows);
+    const uint32_t rows = min(a.rows - r0, static_cast<uint32_t>(kSmallRows));
+    const bool teaching = (Backward || a.loss) && a.entries > 0;
+    if (teaching) {
+        for (int i = tid; i < Slices * kSmallRows * Width; i += kThreads) (&s_table[0][0])[i] = 0.f;
+        const bool slice = wave < Slices;       // wave-uniform; the barriers stand outside its branches
+        const uint32_t r = r0 + min(static_cast<uint32_t>(lane), rows - 1);     // lanes past the last row: the last again
+        const int span = (a.entries + Slices - 1) / Slices, k0 = wave * span, k1 = slice ? min(a.entries, k0 + span) : 0;
+        uint64_t bits = ~uint64_t(0);
+        if (a.mask.data) {
+            const uint32_t *words = reinterpret_cast<const uint32_t *>(row_at(a.mask, r));
+            bits = a.vocab > 32 ? words[0] | static_cast<uint64_t>(words[1]) << 32 : words[0];
+        }
+        const char *ids = row_at(a.ids, r), *teacher = row_at(a.teacher, r);
+        int32_t id[Batch];
+        float t[Batch];
+        // the entries k to k + Batch of the slice; the second pass over a slice of one batch keeps them
+        const auto load = [&](int k) {
+#pragma unroll
+            for (int i = 0; i < Batch; ++i) {
+                const uint64_t at = static_cast<uint32_t>(min(k + i, k1 - 1));
+                id[i] = small_id(ids + at * a.id_step, a.id_type, a.vocab);
+                t[i] = small_float(teacher + at * a.teacher_step, a.teacher_type);
+            }
+#pragma unroll
+            for (int i = 0; i < Batch; ++i)
+                if (k + i >= k1 || t[i] == -INFINITY || (id[i] >= 0 && !(bits >> id[i] & 1))) id[i] = -1;
+        };
+        float m = -INFINITY;
+        for (int k = k0; k < k1; k += Batch) {
+            load(k);
+#pragma unroll
+            for (int i = 0; i < Batch; ++i)
+                if (id[i] >= 0) m = fmaxf(m, fmaxf(t[i], -3.4028235e38f));      // a NaN that counts is no -infinity
+        }
+        if (slice) s_max[wave][lane] = m;
+        __syncthreads();
+        for (int s = 0; s < Slices; ++s) m = fmaxf(m, s_max[s][lane]);
+        float total = 0.f;
+        for (int k = k0; k < k1; k += Batch) {
+            if (span > Batch) load(k);
+#pragma unroll
+            for (int i = 0; i < Batch; ++i) {
+                if (id[i] < 0) continue;
+                const float w = exp2_fast((t[i] - m) * a.log2e_tau);
+                total += w;
+                __hip_atomic_fetch_add(&s_table[wave][lane * Width + id[i]], w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+        }
+        if (slice) s_sum[wave][lane] = total;
+        __syncthreads();
+    }
+    const int lanes = 1 << a.lg, v = (tid & (lanes - 1)) * 4;
+    for (int base = 0; base < kSmallRows; base += kThreads >> a.lg) {
+        const uint32_t local = base + (tid >> a.lg);
+        if (local >= rows) break;       // whole groups
+        const uint32_t r = r0 + local;
+        const bool mine = v < a.vocab;
+        float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        uint32_t bits = 0;
+        if (mine) {
+            load_four(reinterpret_cast<const T *>(row_at(a.logits, r)), v, a.vocab, x);
+            bits = mask_bits<4>(a.mask.data ? reinterpret_cast<const uint32_t *>(row_at(a.mask, r)) : nullptr, v, a.vocab);
+            for (int j = 0; j < 4; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
+        }
+        float p[4] = {0.f, 0.f, 0.f, 0.f};
+        bool has = false;
+        if (teaching) {
+            float total = 0.f;
+            for (int s = 0; s < Slices; ++s) {
+                total += s_sum[s][local];
+                has = has || s_max[s][local] > -INFINITY;
+            }
+            if (mine && has) {
+                const float share = 1.f / total;
+                for (int j = 0; j < 4; ++j) {
+                    if (v + j >= a.vocab) continue;
+                    for (int s = 0; s < Slices; ++s) p[j] += s_table[s][local * Width + v + j];
+                    p[j] = p[j] * share;
+                }
+            }
+        }
+        float m, s, e[4];
+        if (Forward) m = group_max(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), a.lg);
+        else m = reinterpret_cast<const float *>(row_at(a.stats, r))[0];
+        m = Forward && !(m > -INFINITY) ? -INFINITY : m;        // a row of NaN alone
+        // what every exponent is measured from; where a row has no entry above -infinity the sum is 0 and
+        // the distribution NaN
+        for (int j = 0; j < 4; ++j) e[j] = exp2_fast((x[j] - origin(m)) * a.log2e_tau);
+        if (Forward) s = group_sum((e[0] + e[1]) + (e[2] + e[3]), a.lg);
+        else s = reinterpret_cast<const float *>(row_at(a.stats, r))[1];
+        if (Forward && a.stats_out && v == 0) {
+            float *to = reinterpret_cast<float *>(a.stats_out + static_cast<uint64_t>(r) * a.stats_stride);
+            to[0] = m;
+            to[1] = s;
+        }
+        if (Forward && a.loss) {
+            const float log_s = logf(s);
+            float loss = 0.f;
+            for (int j = 0; j < 4; ++j)
+                if (p[j] != 0.f) loss += p[j] * (log_s - (x[j] - m) * a.inv_tau);
+            loss = group_sum(loss, a.lg) * a.tau * a.tau;
+            if (v == 0) *reinterpret_cast<float *>(a.loss + static_cast<uint64_t>(r) * a.loss_stride) = has ? loss : 0.f;
+        }
+        if (Backward && mine) {
+            const float rate = (a.scale.data ? *reinterpret_cast<const float *>(row_at(a.scale, r)) : 1.f) * a.tau;
+            const float share = m > -INFINITY || m != m ? 1.f / s : NAN;
+            for (int j = 0; j < 4; ++j) {
+                const float q = e[j] * share;
+                x[j] = has && (bits >> j & 1) ? rate * (q - p[j]) : 0.f;
+            }
+            store_chunk(reinterpret_cast<O *>(a.grad + static_cast<uint64_t>(r) * a.grad_stride), v, a.vocab, x);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------ launches
 
 // The parts of a row of the forward pass: of whole 8,192 entries, as many as bring 2,048 workgroups (8 a
@@ -397,6 +551,49 @@ int64_t distill_bytes(int64_t rows, int64_t vocab) {
     return partial_bytes(rows, vocab) + (vocab > resident(EMO_F32) ? rows * static_cast<int64_t>(sizeof(float2)) : 0);
 }
 
+// Whether small_kernel takes the rows: of at most 64 entries, strides below 4 GiB.
+bool small_rows(const DistillArgs &a, int32_t grad_size, SmallArgs *s) {
+    constexpr int64_t most = int64_t(1) << 32;
+    const int64_t id_step = a.ids.col_stride * size_of(a.ids.dtype), teacher_step = a.teacher.col_stride * size_of(a.teacher.dtype);
+    if (a.vocab > 64 || a.loss_stride * 4 >= most || a.stats_stride * 4 >= most || a.grad_stride * grad_size >= most || id_step >= most ||
+        teacher_step >= most)
+        return false;
+    *s = {};
+    while ((4 << s->lg) < a.vocab) ++s->lg;
+    s->vocab = a.vocab;
+    s->entries = a.entries;
+    s->rows = a.rows;
+    s->inv_tau = a.inv_tau;
+    s->tau = a.tau;
+    s->log2e_tau = a.log2e_tau;
+    s->id_step = static_cast<uint32_t>(id_step);
+    s->teacher_step = static_cast<uint32_t>(teacher_step);
+    s->id_type = a.ids.dtype;
+    s->teacher_type = a.teacher.dtype;
+    s->loss = a.loss;
+    s->stats_out = a.stats_out;
+    s->grad = a.grad;
+    s->loss_stride = static_cast<uint32_t>(a.loss_stride * 4);
+    s->stats_stride = static_cast<uint32_t>(a.stats_stride * 4);
+    s->grad_stride = static_cast<uint32_t>(a.grad_stride * grad_size);
+    return narrow(a.logits, &s->logits) && narrow(a.ids, &s->ids) && narrow(a.teacher, &s->teacher) && narrow(a.mask, &s->mask) &&
+           narrow(a.scale, &s->scale) && narrow(a.stats, &s->stats);
+}
+
+// Tables of 4 slices of the list, or of 2 for rows of more than 32 entries (34 KB either way: four
+// workgroups a compute unit).
+template <typename T, typename O, bool Forward, bool Backward>
+void launch_small(const SmallArgs &s, hipStream_t st) {
+    in_launches((static_cast<int64_t>(s.rows) + kSmallRows - 1) / kSmallRows, [&](int64_t first, unsigned count) {
+        if (s.vocab <= 16)
+            hipLaunchKernelGGL((small_kernel<T, O, 4, 16, Forward, Backward>), dim3(count), dim3(kThreads), 0, st, s, first);
+        else if (s.vocab <= 32)
+            hipLaunchKernelGGL((small_kernel<T, O, 4, 32, Forward, Backward>), dim3(count), dim3(kThreads), 0, st, s, first);
+        else
+            hipLaunchKernelGGL((small_kernel<T, O, 2, 64, Forward, Backward>), dim3(count), dim3(kThreads), 0, st, s, first);
+    });
+}
+
 unsigned teacher_lds(const DistillArgs &a) { return static_cast<unsigned>((a.entries + 3) / 4 * 4 * kTeacherBytes); }
 
 struct ForwardLaunch {
@@ -406,6 +603,8 @@ struct ForwardLaunch {
 
     template <typename T, typename>
     void run() const {
+        SmallArgs small;
+        if (small_rows(a, 4, &small)) return launch_small<T, float, true, false>(small, st);
         const Parts p = forward_parts(a.rows, a.vocab);
         in_pieces(a.rows, p.parts, [&](uint32_t first, unsigned count, const Pieces &pieces) {
             if (a.vocab <= 2048)
@@ -434,6 +633,8 @@ struct BackwardLaunch {
 
     template <typename T, typename O>
     void run() const {
+        SmallArgs small;
+        if (small_rows(a, sizeof(O), &small)) return launch_small<T, O, false, true>(small, st);
         if (a.vocab <= 2048) tiles<T, O, 64>();
         else tiles<T, O, 256>();
     }
@@ -452,6 +653,8 @@ struct StepLaunch {
 
     template <typename T, typename O>
     void run() const {
+        SmallArgs small;
+        if (small_rows(a, sizeof(O), &small)) return launch_small<T, O, true, true>(small, st);
         if (a.vocab <= 2048) rows<T, O, 64, 32>();
         else if (a.vocab <= 8192) rows<T, O, 256, 32>();
         else if (a.vocab <= 32768) rows<T, O, 512, 64>();
