@@ -433,7 +433,7 @@ typedef struct {
  *   out             dense [rows][V], the logits' type or EMO_F32, or NULL.
  *   choice          [rows][1], EMO_U8 (V <= 255), EMO_I32 or EMO_I64, or NULL.
  *   workspace       device memory of at least the bytes emo_adjust_workspace names for this rows and
- *                   vocab, 16-byte aligned (NULL where that is 0).  Its contents before and after do
+ *                   vocab, 16-byte aligned (NULL where that is 0, as for every vocab <= 2048).  Its contents before and after do
  *                   not matter, but calls that may overlap (on two streams, or in two captured
  *                   graphs) need one each.
  * Asynchronous on `stream`, allocates nothing and may be captured.

@@ -369,8 +369,8 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
 
 // Rows of at most 64 entries: 64 rows a workgroup, in two phases.  The teacher's: a lane per row and a wave per
 // slice of the list, so that level bytes [K][rows] come 64 to a load; each lane adds its slice's weights to
-// its row's table in LDS, entry by entry in the list's order (no two lanes share a table: a fixed order
-// without comparing ids, K adds where K^2 comparisons bounded the call).  The student's: a group of 2^lg
+// its row's table in LDS in the list's order (no two lanes share a table: a fixed order without comparing
+// all ids with each other; reads and stores four at a time, as LDS's own float additions took 0.3 us each).  The student's: a group of 2^lg
 // lanes per row, four entries a lane.
 struct SmallArgs {
     int32_t lg, vocab, entries;
@@ -385,138 +385,203 @@ struct SmallArgs {
 
 constexpr int kSmallRows = 64;
 
-__device__ __forceinline__ int32_t small_id(const char *p, int32_t type, int32_t vocab) {
-    int64_t id;
-    if (type == EMO_U8) id = *reinterpret_cast<const uint8_t *>(p);
-    else if (type == EMO_I32) id = *reinterpret_cast<const int32_t *>(p);
-    else id = *reinterpret_cast<const int64_t *>(p);
-    return id >= 0 && id < vocab ? static_cast<int32_t>(id) : -1;
+// Loads entries k to k + Batch of a row's list, those from k1 on repeating the last: get(i, address) for each, in
+// flight together, at a scalar address plus the row's 32-bit offset.  The scalar part is opaque, or the
+// compiler adds the row's offset first and multiplies in vector registers, at a quarter of their rate.
+template <int Batch, typename F>
+__device__ __forceinline__ void small_entries(const char *list, uint32_t row, uint32_t step, int k, int k1, const F &get) {
+    const char *p = list + static_cast<uint64_t>(static_cast<uint32_t>(k)) * step;
+#pragma unroll
+    for (int i = 0; i < Batch; ++i) {
+        const uint64_t here = reinterpret_cast<uint64_t>(p);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(here));
+        const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(here >> 32));
+        p = reinterpret_cast<const char *>(static_cast<uint64_t>(hi) << 32 | lo);
+        get(i, p + row);
+        p += k + i + 1 < k1 ? step : 0;
+    }
 }
 
-__device__ __forceinline__ float small_float(const char *p, int32_t type) {
-    if (type == EMO_F32) return *reinterpret_cast<const float *>(p);
-    if (type == EMO_F16) return static_cast<float>(*reinterpret_cast<const _Float16 *>(p));
-    return static_cast<float>(*reinterpret_cast<const __bf16 *>(p));
+// An id that is no index is 2^31 - 1 or more.  The type is looked at once: a branch an entry would wait for each.
+template <int Batch>
+__device__ __forceinline__ void small_ids(const char *ids, uint32_t row, uint32_t step, int32_t type, int k, int k1, uint32_t (&id)[Batch]) {
+    if (type == EMO_U8) {
+        small_entries<Batch>(ids, row, step, k, k1, [&](int i, const char *p) { id[i] = *reinterpret_cast<const uint8_t *>(p); });
+    } else if (type == EMO_I32) {
+        small_entries<Batch>(ids, row, step, k, k1, [&](int i, const char *p) { id[i] = *reinterpret_cast<const uint32_t *>(p); });
+    } else {
+        uint64_t wide[Batch];
+        small_entries<Batch>(ids, row, step, k, k1, [&](int i, const char *p) { wide[i] = *reinterpret_cast<const uint64_t *>(p); });
+#pragma unroll
+        for (int i = 0; i < Batch; ++i) id[i] = static_cast<uint32_t>(wide[i] < 0x7fffffffu ? wide[i] : 0x7fffffffu);
+    }
+}
+
+template <int Batch>
+__device__ __forceinline__ void small_floats(const char *from, uint32_t row, uint32_t step, int32_t type, int k, int k1, float (&t)[Batch]) {
+    if (type == EMO_F32) {
+        small_entries<Batch>(from, row, step, k, k1, [&](int i, const char *p) { t[i] = *reinterpret_cast<const float *>(p); });
+    } else {
+        uint16_t half[Batch];
+        small_entries<Batch>(from, row, step, k, k1, [&](int i, const char *p) { half[i] = *reinterpret_cast<const uint16_t *>(p); });
+#pragma unroll
+        for (int i = 0; i < Batch; ++i)
+            t[i] = type == EMO_F16 ? static_cast<float>(__builtin_bit_cast(_Float16, half[i])) : __uint_as_float(static_cast<uint32_t>(half[i]) << 16);
+    }
 }
 
 template <typename T, typename O, int Slices, int Most, bool Forward, bool Backward>
 __global__ void __launch_bounds__(kThreads) small_kernel(SmallArgs a, int64_t first) {
     constexpr int Width = Most + 1, Batch = 16;     // a table's rows start in different banks
-    __shared__ float s_table[Slices][kSmallRows * Width];
+    constexpr int Turns = Most / 16;                // rows that a group of lanes takes
+    __shared__ alignas(16) float s_table[Slices * kSmallRows * Width];
     __shared__ float s_max[Slices][kSmallRows], s_sum[Slices][kSmallRows];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const uint32_t r0 = static_cast<uint32_t>((first + blockIdx.x) * kSmallRows);
     const uint32_t rows = min(a.rows - r0, static_cast<uint32_t>(kSmallRows));
     const bool teaching = (Backward || a.loss) && a.entries > 0;
+
+    // the student's loads are in flight over the teacher's phase
+    const int v = (tid & ((1 << a.lg) - 1)) * 4;
+    const bool mine = v < a.vocab;
+    float x[Turns][4], m[Turns], s[Turns], rate[Turns];
+    uint32_t bits[Turns];
+#pragma unroll
+    for (int u = 0; u < Turns; ++u) {
+        const uint32_t local = u * (kThreads >> a.lg) + (tid >> a.lg);
+        const uint32_t r = r0 + min(local, rows - 1);       // rows past the last: the last again
+        for (int j = 0; j < 4; ++j) x[u][j] = -INFINITY;
+        bits[u] = 0;
+        if (mine) {
+            load_four(reinterpret_cast<const T *>(row_at(a.logits, r)), v, a.vocab, x[u]);
+            bits[u] = mask_bits<4>(a.mask.data ? reinterpret_cast<const uint32_t *>(row_at(a.mask, r)) : nullptr, v, a.vocab);
+        }
+        if (Backward) rate[u] = a.scale.data ? *reinterpret_cast<const float *>(row_at(a.scale, r)) : 1.f;
+        if (!Forward) {
+            m[u] = reinterpret_cast<const float *>(row_at(a.stats, r))[0];
+            s[u] = reinterpret_cast<const float *>(row_at(a.stats, r))[1];
+        }
+    }
+
     if (teaching) {
-        for (int i = tid; i < Slices * kSmallRows * Width; i += kThreads) (&s_table[0][0])[i] = 0.f;
-        const bool slice = wave < Slices;       // wave-uniform; the barriers stand outside its branches
-        const uint32_t r = r0 + min(static_cast<uint32_t>(lane), rows - 1);     // lanes past the last row: the last again
+        const bool slice = wave < Slices;       // the barriers stand outside the branches
+        const uint32_t r = r0 + min(static_cast<uint32_t>(lane), rows - 1);
         const int span = (a.entries + Slices - 1) / Slices, k0 = wave * span, k1 = slice ? min(a.entries, k0 + span) : 0;
-        uint64_t bits = ~uint64_t(0);
+        const uint32_t id_row = row_index32(a.ids, r) * a.ids.stride, teacher_row = row_index32(a.teacher, r) * a.teacher.stride;
+        using Open = typename std::conditional<Most <= 32, uint32_t, uint64_t>::type;
+        Open open = ~Open(0);       // the ids that count
         if (a.mask.data) {
             const uint32_t *words = reinterpret_cast<const uint32_t *>(row_at(a.mask, r));
-            bits = a.vocab > 32 ? words[0] | static_cast<uint64_t>(words[1]) << 32 : words[0];
+            open = words[0];
+            if (Most > 32 && a.vocab > 32) open |= static_cast<Open>(static_cast<uint64_t>(words[1]) << 32);
         }
-        const char *ids = row_at(a.ids, r), *teacher = row_at(a.teacher, r);
-        int32_t id[Batch];
-        float t[Batch];
-        // the entries k to k + Batch of the slice; the second pass over a slice of one batch keeps them
+        if (a.vocab < static_cast<int>(8 * sizeof(Open))) open &= (Open(1) << a.vocab) - 1;
+        uint32_t id[Batch];
+        float t[Batch];     // -infinity where the entry does not count; its id then is the place behind the table's row
         const auto load = [&](int k) {
+            small_ids<Batch>(a.ids.data, id_row, a.id_step, a.id_type, k, k1, id);
+            small_floats<Batch>(a.teacher.data, teacher_row, a.teacher_step, a.teacher_type, k, k1, t);
 #pragma unroll
             for (int i = 0; i < Batch; ++i) {
-                const uint64_t at = static_cast<uint32_t>(min(k + i, k1 - 1));
-                id[i] = small_id(ids + at * a.id_step, a.id_type, a.vocab);
-                t[i] = small_float(teacher + at * a.teacher_step, a.teacher_type);
+                const bool counts = id[i] < 8 * sizeof(Open) && k + i < k1 && (open >> (id[i] % (8 * sizeof(Open))) & 1);
+                t[i] = counts ? t[i] : -INFINITY;
+                id[i] = counts ? id[i] : Most;
             }
-#pragma unroll
-            for (int i = 0; i < Batch; ++i)
-                if (k + i >= k1 || t[i] == -INFINITY || (id[i] >= 0 && !(bits >> id[i] & 1))) id[i] = -1;
         };
-        float m = -INFINITY;
+        for (int i = tid * 4; i < Slices * kSmallRows * Width; i += kThreads * 4)
+            *reinterpret_cast<float4 *>(s_table + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = -INFINITY;
+        bool nan = false;
         for (int k = k0; k < k1; k += Batch) {
             load(k);
 #pragma unroll
-            for (int i = 0; i < Batch; ++i)
-                if (id[i] >= 0) m = fmaxf(m, fmaxf(t[i], -3.4028235e38f));      // a NaN that counts is no -infinity
-        }
-        if (slice) s_max[wave][lane] = m;
-        __syncthreads();
-        for (int s = 0; s < Slices; ++s) m = fmaxf(m, s_max[s][lane]);
-        float total = 0.f;
-        for (int k = k0; k < k1; k += Batch) {
-            if (span > Batch) load(k);
-#pragma unroll
             for (int i = 0; i < Batch; ++i) {
-                if (id[i] < 0) continue;
-                const float w = exp2_fast((t[i] - m) * a.log2e_tau);
-                total += w;
-                __hip_atomic_fetch_add(&s_table[wave][lane * Width + id[i]], w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                top = fmaxf(top, t[i]);
+                nan = nan || t[i] != t[i];
+            }
+        }
+        if (slice) s_max[wave][lane] = nan ? INFINITY : top;     // where every exponential comes out as NaN
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < Slices; ++q) top = fmaxf(top, s_max[q][lane]);
+        top = origin(top);
+        float total = 0.f;
+        float *table = s_table + (wave % Slices * kSmallRows + lane) * Width;
+        for (int k = k0; k < k1; k += Batch) {
+            if (span > Batch) load(k);      // a slice of one batch is still there
+#pragma unroll
+            for (int i = 0; i < Batch; i += 4) {
+                // four entries at once: the later of equal ids adds to the earlier's sum, and is stored after it
+                float w[4], sum[4];
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = exp2_fast((t[i + j] - top) * a.log2e_tau);
+                    total += w[j];
+                    sum[j] = table[id[i + j]];
+                }
+                for (int j = 0; j < 4; ++j) {
+                    for (int b = 0; b < j; ++b) sum[j] = id[i + j] == id[i + b] ? sum[b] : sum[j];
+                    sum[j] += w[j];
+                }
+                for (int j = 0; j < 4; ++j) table[id[i + j]] = sum[j];
             }
         }
         if (slice) s_sum[wave][lane] = total;
         __syncthreads();
     }
-    const int lanes = 1 << a.lg, v = (tid & (lanes - 1)) * 4;
-    for (int base = 0; base < kSmallRows; base += kThreads >> a.lg) {
-        const uint32_t local = base + (tid >> a.lg);
+
+#pragma unroll
+    for (int u = 0; u < Turns; ++u) {
+        const uint32_t local = u * (kThreads >> a.lg) + (tid >> a.lg);
         if (local >= rows) break;       // whole groups
         const uint32_t r = r0 + local;
-        const bool mine = v < a.vocab;
-        float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        uint32_t bits = 0;
-        if (mine) {
-            load_four(reinterpret_cast<const T *>(row_at(a.logits, r)), v, a.vocab, x);
-            bits = mask_bits<4>(a.mask.data ? reinterpret_cast<const uint32_t *>(row_at(a.mask, r)) : nullptr, v, a.vocab);
-            for (int j = 0; j < 4; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
-        }
+        for (int j = 0; j < 4; ++j) x[u][j] = bits[u] >> j & 1 ? x[u][j] : -INFINITY;
         float p[4] = {0.f, 0.f, 0.f, 0.f};
         bool has = false;
         if (teaching) {
             float total = 0.f;
-            for (int s = 0; s < Slices; ++s) {
-                total += s_sum[s][local];
-                has = has || s_max[s][local] > -INFINITY;
+#pragma unroll
+            for (int q = 0; q < Slices; ++q) {
+                total += s_sum[q][local];
+                has = has || s_max[q][local] > -INFINITY;
             }
             if (mine && has) {
-                const float share = 1.f / total;
+                const float share = __builtin_amdgcn_rcpf(total);
                 for (int j = 0; j < 4; ++j) {
                     if (v + j >= a.vocab) continue;
-                    for (int s = 0; s < Slices; ++s) p[j] += s_table[s][local * Width + v + j];
+#pragma unroll
+                    for (int q = 0; q < Slices; ++q) p[j] += s_table[(q * kSmallRows + local) * Width + v + j];
                     p[j] = p[j] * share;
                 }
             }
         }
-        float m, s, e[4];
-        if (Forward) m = group_max(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), a.lg);
-        else m = reinterpret_cast<const float *>(row_at(a.stats, r))[0];
-        m = Forward && !(m > -INFINITY) ? -INFINITY : m;        // a row of NaN alone
-        // what every exponent is measured from; where a row has no entry above -infinity the sum is 0 and
-        // the distribution NaN
-        for (int j = 0; j < 4; ++j) e[j] = exp2_fast((x[j] - origin(m)) * a.log2e_tau);
-        if (Forward) s = group_sum((e[0] + e[1]) + (e[2] + e[3]), a.lg);
-        else s = reinterpret_cast<const float *>(row_at(a.stats, r))[1];
+        if (Forward) {
+            m[u] = group_max(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])), a.lg);
+            if (!(m[u] > -INFINITY)) m[u] = -INFINITY;      // a row of NaN alone
+        }
+        float e[4];
+        for (int j = 0; j < 4; ++j) e[j] = exp2_fast((x[u][j] - origin(m[u])) * a.log2e_tau);
+        if (Forward) s[u] = group_sum((e[0] + e[1]) + (e[2] + e[3]), a.lg);
         if (Forward && a.stats_out && v == 0) {
             float *to = reinterpret_cast<float *>(a.stats_out + static_cast<uint64_t>(r) * a.stats_stride);
-            to[0] = m;
-            to[1] = s;
+            to[0] = m[u];
+            to[1] = s[u];
         }
         if (Forward && a.loss) {
-            const float log_s = logf(s);
+            const float log_s = 0.69314718f * __builtin_amdgcn_logf(s[u]);
             float loss = 0.f;
             for (int j = 0; j < 4; ++j)
-                if (p[j] != 0.f) loss += p[j] * (log_s - (x[j] - m) * a.inv_tau);
+                if (p[j] != 0.f) loss += p[j] * (log_s - (x[u][j] - m[u]) * a.inv_tau);
             loss = group_sum(loss, a.lg) * a.tau * a.tau;
             if (v == 0) *reinterpret_cast<float *>(a.loss + static_cast<uint64_t>(r) * a.loss_stride) = has ? loss : 0.f;
         }
         if (Backward && mine) {
-            const float rate = (a.scale.data ? *reinterpret_cast<const float *>(row_at(a.scale, r)) : 1.f) * a.tau;
-            const float share = m > -INFINITY || m != m ? 1.f / s : NAN;
+            // a row without an entry above -infinity has no distribution
+            const float share = m[u] > -INFINITY || m[u] != m[u] ? __builtin_amdgcn_rcpf(s[u]) : NAN;
             for (int j = 0; j < 4; ++j) {
                 const float q = e[j] * share;
-                x[j] = has && (bits >> j & 1) ? rate * (q - p[j]) : 0.f;
+                x[u][j] = has && (bits[u] >> j & 1) ? rate[u] * a.tau * (q - p[j]) : 0.f;
             }
-            store_chunk(reinterpret_cast<O *>(a.grad + static_cast<uint64_t>(r) * a.grad_stride), v, a.vocab, x);
+            store_chunk(reinterpret_cast<O *>(a.grad + static_cast<uint64_t>(r) * a.grad_stride), v, a.vocab, x[u]);
         }
     }
 }
@@ -551,12 +616,15 @@ int64_t distill_bytes(int64_t rows, int64_t vocab) {
     return partial_bytes(rows, vocab) + (vocab > resident(EMO_F32) ? rows * static_cast<int64_t>(sizeof(float2)) : 0);
 }
 
-// Whether small_kernel takes the rows: of at most 64 entries, strides below 4 GiB.
+// Bytes from an operand's first row to its last.
+int64_t extent(const Mat &m) { return m.rows > 1 ? static_cast<int64_t>(m.rows - 1) * m.row_stride * size_of(m.dtype) : 0; }
+
+// Whether small_kernel takes the rows: of at most 64 entries, strides and the lists' extents below 4 GiB.
 bool small_rows(const DistillArgs &a, int32_t grad_size, SmallArgs *s) {
     constexpr int64_t most = int64_t(1) << 32;
     const int64_t id_step = a.ids.col_stride * size_of(a.ids.dtype), teacher_step = a.teacher.col_stride * size_of(a.teacher.dtype);
     if (a.vocab > 64 || a.loss_stride * 4 >= most || a.stats_stride * 4 >= most || a.grad_stride * grad_size >= most || id_step >= most ||
-        teacher_step >= most)
+        teacher_step >= most || extent(a.ids) >= most || extent(a.teacher) >= most)
         return false;
     *s = {};
     while ((4 << s->lg) < a.vocab) ++s->lg;
@@ -658,8 +726,9 @@ struct StepLaunch {
         if (a.vocab <= 2048) rows<T, O, 64, 32>();
         else if (a.vocab <= 8192) rows<T, O, 256, 32>();
         else if (a.vocab <= 32768) rows<T, O, 512, 64>();
-        else if (a.vocab <= 65536) rows<T, O, 1024, 64>();
-        else if constexpr (sizeof(T) == 2) rows<T, O, 1024, 128>();
+        else if constexpr (sizeof(T) == 4) rows<T, O, 1024, 64>();
+        else if (a.vocab <= 65536) rows<T, O, 512, 128>();
+        else rows<T, O, 1024, 128>();
     }
 };
 

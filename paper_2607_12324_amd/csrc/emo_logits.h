@@ -44,9 +44,12 @@ struct Rows {
     uint32_t stride, rows, magic, shift;
 };
 
+__device__ __forceinline__ uint32_t row_index32(const Rows &m, uint32_t r) {
+    return m.magic ? r - (__umulhi(r, m.magic) >> m.shift) * m.rows : r;
+}
+
 __device__ __forceinline__ const char *row_at(const Rows &m, uint32_t r) {
-    if (m.magic) r -= (__umulhi(r, m.magic) >> m.shift) * m.rows;
-    return m.data + static_cast<uint64_t>(r) * m.stride;
+    return m.data + static_cast<uint64_t>(row_index32(m, r)) * m.stride;
 }
 
 // The workgroups of rows of `parts` pieces: workgroup b < 2^31 of a launch takes piece b % parts of the

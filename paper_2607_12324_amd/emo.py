@@ -8,7 +8,9 @@ raises at import time; there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -409,154 +411,170 @@ def select_from_results_noalloc(makespan, energy, latency_target: float, mask, r
 
 
 _DTYPES: dict = {}      # torch type -> emo_dtype
+_TENSOR = struct.Struct("@P4q2i").pack      # an emo_tensor (Tensor), as bytes: a quarter of its ctypes call
 
 
-def _operand(t, name: str, device, column: bool = False):
-    """emo_tensor of a device tensor [rows, n], by reference; a 1-D tensor is one row, or with
-    `column` one value per row.  None stays None."""
-    if t is None:
-        return None
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the logits are on {device}")
+def _operand(t, name: str, index: int):
+    """emo_tensor of a tensor [rows, n] on device `index`, or of one row [n]."""
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the logits are on cuda:{index}")
     dtype = _DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{name} has the type {t.dtype}, which no call takes")
-    shape, stride = t.shape, t.stride()
-    if column:
-        if len(shape) != 1:
-            raise ValueError(f"{name} must be [rows], one value per row")
-        return ctypes.byref(Tensor(t.data_ptr(), shape[0], 1, stride[0], 1, dtype, 0))
+    shape = t.shape
     if len(shape) == 2:
-        return ctypes.byref(Tensor(t.data_ptr(), shape[0], shape[1], stride[0], stride[1], dtype, 0))
-    if len(shape) == 1:
-        return ctypes.byref(Tensor(t.data_ptr(), 1, shape[0], 0, stride[0], dtype, 0))
-    raise ValueError(f"{name} must have one or two dimensions")
+        rs, cs = t.stride()
+        return _TENSOR(t.data_ptr(), shape[0], shape[1], rs, cs, dtype, 0)
+    if len(shape) != 1:
+        raise ValueError(f"{name} must have one or two dimensions")
+    return _TENSOR(t.data_ptr(), 1, shape[0], 0, t.stride()[0], dtype, 0)
+
+
+def _column(t, name: str, index: int):
+    """emo_tensor of a tensor [rows], one value per row."""
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the logits are on cuda:{index}")
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise ValueError(f"{name} has the type {t.dtype}, which no call takes")
+    if len(t.shape) != 1:
+        raise ValueError(f"{name} must be [rows], one value per row")
+    return _TENSOR(t.data_ptr(), t.shape[0], 1, t.stride()[0], 1, dtype, 0)
 
 
 def _logits_shape(logits):
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
-                        torch.int64: 5})
     shape = logits.shape
     if len(shape) != 2:
         raise ValueError("logits must be [rows, entries]")
     if not logits.is_cuda:
         raise ValueError("logits must be a device tensor")
-    return shape[0], shape[1], logits.device
-
-
-class _Place:
-    """Where a call on logits runs: their device made current, and a stream of it (the current one, or
-    the one given).  Tensors that the call makes belong to that stream, so a captured call owns its
-    workspace and a reused one is free of the calls before it."""
-
-    def __init__(self, device, stream):
+    if not _DTYPES:
         import torch
-        if stream is not None and stream.device != device:
-            raise ValueError(f"the stream is on {stream.device}, the logits are on {device}")
-        self._torch, self.device, self._guard = torch, device, None
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
+                        torch.int64: 5})
+        global _torch, _device, _raw_stream
+        _torch = torch
+        _device = torch._C._cuda_getDevice
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return shape[0], shape[1], logits.get_device()
+
+
+def _placed(call):
+    """Makes the logits' device and the given stream current for a call on logits.  Tensors that the call
+    makes (outputs, workspace) then belong to its stream: a captured call owns its workspace, and a
+    reused one is free of the calls before it."""
+    @functools.wraps(call)
+    def placed(logits, *args, stream=None, **kw):
+        _, _, index = _logits_shape(logits)
         if stream is not None:
-            self._guard = torch.cuda.stream(stream)
-        elif device.index != torch.cuda.current_device():
-            self._guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
-
-    def empty(self, shape, dtype=None):
-        return self._torch.empty(shape, dtype=dtype or self._torch.float32, device=self.device)
-
-    def workspace(self, given, size_call, rows: int, vocab: int):
-        """(pointer, bytes, tensor) of the workspace a call needs: the given one, or one made here."""
-        n = ctypes.c_int64(0)
-        _check(size_call(rows, vocab, ctypes.byref(n)))
-        if given is None:
-            if n.value == 0:
-                return None, 0, None
-            given = self.empty(n.value, self._torch.uint8)
-        if given.device != self.device or not given.is_contiguous():
-            raise ValueError("workspace must be contiguous and on the logits' device")
-        return given.data_ptr(), given.numel() * given.element_size(), given
+            if stream.device != logits.device:
+                raise ValueError(f"the stream is on {stream.device}, the logits are on {logits.device}")
+            with _torch.cuda.stream(stream):
+                return call(logits, *args, **kw)
+        if index != _device():
+            with _torch.cuda.device(index):
+                return call(logits, *args, **kw)
+        return call(logits, *args, **kw)
+    return placed
 
 
+def _workspace(given, size_call, rows: int, vocab: int, logits):
+    """(pointer, bytes, tensor) of the workspace a call needs: the given one, or one made here."""
+    if vocab <= 2048:       # no call on shorter rows needs one
+        return None, 0, None
+    n = ctypes.c_int64(0)
+    _check(size_call(rows, vocab, ctypes.byref(n)))
+    if given is None:
+        if n.value == 0:
+            return None, 0, None
+        given = _torch.empty(n.value, dtype=_torch.uint8, device=logits.device)
+    if given.device != logits.device or not given.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the logits' device")
+    return given.data_ptr(), given.numel() * given.element_size(), given
+
+
+@_placed
 def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None, repetition=None,
                   frequency=None, presence=None, bias=None, inv_temperature=None, mask=None, noise=None,
-                  out=None, choice=None, workspace=None, stream=None):
+                  out=None, choice=None, workspace=None):
     """Penalties, bias, temperature and mask on rows of logits, and a choice from them
     (emo_adjust_logits).  Returns (out, choice): what was given; the adjusted logits are allocated
     (in the logits' type) when neither is.
 
     logits [n, V]; history [n, L] ids; lengths, repetition, frequency, presence, inv_temperature [n];
     bias, noise [n, V] or [V]; mask [n, (V + 31) // 32] or one row, int32 words; out [rows, V]; choice
-    [rows] uint8, int32 or int64.  Row r reads row r % n of each; rows defaults to the logits' n."""
-    n, V, dev = _logits_shape(logits)
-    rows = n if rows is None else int(rows)
-    with _Place(dev, stream) as at:
-        if out is None and choice is None:
-            out = at.empty((rows, V), logits.dtype)
-        ws, size, _keep = (None, 0, None) if choice is None else at.workspace(workspace, lib.emo_adjust_workspace, rows, V)
-        _check(lib.emo_adjust_logits(
-            rows, V, _operand(logits, "logits", dev), _operand(history, "history", dev),
-            _operand(lengths, "lengths", dev, True), _operand(repetition, "repetition", dev, True),
-            _operand(frequency, "frequency", dev, True), _operand(presence, "presence", dev, True),
-            _operand(bias, "bias", dev), _operand(inv_temperature, "inv_temperature", dev, True),
-            _operand(mask, "mask", dev), _operand(noise, "noise", dev), _operand(out, "out", dev),
-            _operand(choice, "choice", dev, True), ws, size, _stream(None)))
+    [rows] uint8, int32 or int64.  Row r reads row r % n of each; rows defaults to the logits' n.
+    `stream`: the stream to run on (default: the current one of the logits' device)."""
+    n, V, index = _logits_shape(logits)
+    if rows is None:
+        rows = n
+    if out is None and choice is None:
+        out = _torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
+    ws, size, _keep = (None, 0, None) if choice is None else _workspace(workspace, lib.emo_adjust_workspace, rows, V, logits)
+    _check(lib.emo_adjust_logits(
+        rows, V, _operand(logits, "logits", index),
+        None if history is None else _operand(history, "history", index),
+        None if lengths is None else _column(lengths, "lengths", index),
+        None if repetition is None else _column(repetition, "repetition", index),
+        None if frequency is None else _column(frequency, "frequency", index),
+        None if presence is None else _column(presence, "presence", index),
+        None if bias is None else _operand(bias, "bias", index),
+        None if inv_temperature is None else _column(inv_temperature, "inv_temperature", index),
+        None if mask is None else _operand(mask, "mask", index),
+        None if noise is None else _operand(noise, "noise", index),
+        None if out is None else _operand(out, "out", index),
+        None if choice is None else _column(choice, "choice", index),
+        ws, size, _raw_stream(index)))
     return out, choice
 
 
+@_placed
 def distill_forward(logits, ids, teacher, temperature: float = 1.0, *, mask=None, loss=None, stats=None,
-                    workspace=None, stream=None):
+                    workspace=None):
     """Cross entropy of the logits [N, V] against a teacher's top entries (emo_distill_forward):
     ids [n, K], teacher [n, K] or one row each.  Returns (loss [N], stats [N, 2] for the backward
-    pass), allocated when not given.  Autograd does not see it: distill_backward is the gradient."""
-    N, V, dev = _logits_shape(logits)
-    with _Place(dev, stream) as at:
-        loss = at.empty(N) if loss is None else loss
-        stats = at.empty((N, 2)) if stats is None else stats
-        ws, size, _keep = at.workspace(workspace, lib.emo_distill_workspace, N, V)
-        _check(lib.emo_distill_forward(
-            N, V, _operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev),
-            float(temperature), _operand(mask, "mask", dev), _operand(loss, "loss", dev, True),
-            _operand(stats, "stats", dev), ws, size, _stream(None)))
+    pass), allocated when not given.  Autograd does not see it: distill_backward is the gradient.
+    `stream` as in adjust_logits."""
+    N, V, index = _logits_shape(logits)
+    loss = _torch.empty(N, dtype=_torch.float32, device=logits.device) if loss is None else loss
+    stats = _torch.empty((N, 2), dtype=_torch.float32, device=logits.device) if stats is None else stats
+    ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, logits)
+    _check(lib.emo_distill_forward(
+        N, V, _operand(logits, "logits", index), _operand(ids, "ids", index), _operand(teacher, "teacher", index),
+        temperature, None if mask is None else _operand(mask, "mask", index), _column(loss, "loss", index),
+        _operand(stats, "stats", index), ws, size, _raw_stream(index)))
     return loss, stats
 
 
-def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, grad=None,
-                     stream=None):
+@_placed
+def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, grad=None):
     """Gradient [N, V] of sum(scale * loss) by the logits, from the statistics that distill_forward
     returned for the same operands (emo_distill_backward); scale [n] or None (1).  `grad` may be the
-    logits."""
-    N, V, dev = _logits_shape(logits)
-    with _Place(dev, stream) as at:
-        grad = at.empty((N, V), logits.dtype) if grad is None else grad
-        _check(lib.emo_distill_backward(
-            N, V, _operand(logits, "logits", dev), _operand(stats, "stats", dev), _operand(ids, "ids", dev),
-            _operand(teacher, "teacher", dev), float(temperature), _operand(scale, "scale", dev, True),
-            _operand(mask, "mask", dev), _operand(grad, "grad", dev), _stream(None)))
+    logits.  `stream` as in adjust_logits."""
+    N, V, index = _logits_shape(logits)
+    grad = _torch.empty((N, V), dtype=logits.dtype, device=logits.device) if grad is None else grad
+    _check(lib.emo_distill_backward(
+        N, V, _operand(logits, "logits", index), _operand(stats, "stats", index), _operand(ids, "ids", index),
+        _operand(teacher, "teacher", index), temperature, None if scale is None else _column(scale, "scale", index),
+        None if mask is None else _operand(mask, "mask", index), _operand(grad, "grad", index), _raw_stream(index)))
     return grad
 
 
+@_placed
 def distill_step(logits, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, loss=None, grad=None,
-                 workspace=None, stream=None):
+                 workspace=None):
     """Loss [N] and gradient [N, V] in one call (emo_distill_step), for a scale known beforehand (e.g.
-    [1 / N]).  `grad` may be the logits."""
-    N, V, dev = _logits_shape(logits)
-    with _Place(dev, stream) as at:
-        loss = at.empty(N) if loss is None else loss
-        grad = at.empty((N, V), logits.dtype) if grad is None else grad
-        ws, size, _keep = at.workspace(workspace, lib.emo_distill_workspace, N, V)
-        _check(lib.emo_distill_step(
-            N, V, _operand(logits, "logits", dev), _operand(ids, "ids", dev), _operand(teacher, "teacher", dev),
-            float(temperature), _operand(scale, "scale", dev, True), _operand(mask, "mask", dev),
-            _operand(loss, "loss", dev, True), _operand(grad, "grad", dev), ws, size, _stream(None)))
+    [1 / N]).  `grad` may be the logits.  `stream` as in adjust_logits."""
+    N, V, index = _logits_shape(logits)
+    loss = _torch.empty(N, dtype=_torch.float32, device=logits.device) if loss is None else loss
+    grad = _torch.empty((N, V), dtype=logits.dtype, device=logits.device) if grad is None else grad
+    ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, logits)
+    _check(lib.emo_distill_step(
+        N, V, _operand(logits, "logits", index), _operand(ids, "ids", index), _operand(teacher, "teacher", index),
+        temperature, None if scale is None else _column(scale, "scale", index),
+        None if mask is None else _operand(mask, "mask", index), _column(loss, "loss", index),
+        _operand(grad, "grad", index), ws, size, _raw_stream(index)))
     return loss, grad
 
 
