@@ -97,13 +97,36 @@ __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r)
 
 constexpr uint32_t kUnseen = 0xffffffffu;
 
-// A workgroup per tile of Threads * 32 entries of a row.  Bound by memory: a thread's logits (64 or 128
-// bytes) are all in flight before anything else.  While they come, the history's ids in the tile are
-// counted in a table in LDS (a word an entry, kUnseen plus the count; integer atomics: any order gives the
-// same counts), and whoever counts an id first puts the penalised logit in the count's place afterwards:
-// penalties cost a few of the history's ids, not every entry (a division each where any lane of a wave
-// has a seen entry, which is nearly always, took 320 of 700 instructions a chunk).  The choice of a row of
-// several tiles goes through `parts`, one best entry a tile, and choose_kernel.
+// The first Held * Threads ids of a row's history, as they stand (ids of 64 bits cut to -1 where they do not
+// fit 32); -1 from `cols` on.
+template <int Threads, int Held>
+__device__ __forceinline__ void load_history(const Mat &m, uint32_t row, int32_t (&id)[Held]) {
+    const int tid = threadIdx.x;
+    const int64_t base = static_cast<int64_t>(row) * m.row_stride;
+    const auto at = [&](int h) { return base + static_cast<int64_t>(min(tid + h * Threads, m.cols - 1)) * m.col_stride; };
+    if (m.dtype == EMO_U8) {
+#pragma unroll
+        for (int h = 0; h < Held; ++h) id[h] = reinterpret_cast<const uint8_t *>(m.data)[at(h)];
+    } else if (m.dtype == EMO_I32) {
+#pragma unroll
+        for (int h = 0; h < Held; ++h) id[h] = reinterpret_cast<const int32_t *>(m.data)[at(h)];
+    } else {
+        int64_t wide[Held];
+#pragma unroll
+        for (int h = 0; h < Held; ++h) wide[h] = reinterpret_cast<const int64_t *>(m.data)[at(h)];
+#pragma unroll
+        for (int h = 0; h < Held; ++h) id[h] = wide[h] == static_cast<int32_t>(wide[h]) ? static_cast<int32_t>(wide[h]) : -1;
+    }
+}
+
+// A workgroup per tile of Threads * PerThread entries of a row.  Bound by memory and, with a history, by what
+// has to follow each other in a workgroup: so everything that needs nothing is loaded at once (logits, mask,
+// bias, length, the first ids), and one more round trip fetches the logits of the ids in the tile.  The ids
+// are counted in a table in LDS (a word an entry, kUnseen plus the count; integer atomics: any order gives
+// the same counts), and whoever counts an id first puts the penalised logit in the count's place: penalties
+// cost a few of the history's ids, not every entry (a division each where any lane of a wave has a seen
+// entry, which is nearly always, took 320 of 700 instructions a chunk).  The choice of a row of several
+// tiles goes through `parts`, one best entry a tile, and choose_kernel.
 template <typename T, typename O, int Threads, int PerThread, bool History>
 __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint32_t first, Pieces pieces, Best *parts) {
     constexpr int N = kChunk<T>, C = PerThread / N, Tile = Threads * PerThread;
@@ -120,44 +143,70 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
     float x_rest = rest < n ? static_cast<float>(logits[rest]) : 0.f;
     const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) + v0 / 32 : nullptr;
     if (mask) load_mask<T, Threads, C>(mask, whole, bytes);
-    const int32_t L = History ? live_history(a, r) : 0;
     const float inv_t = row_value(a.inv_temperature, r, 1.f);
-    if (History && L > 0) {
+    const float *bias = a.bias.data ? row_of<float>(a.bias, r) + v0 : nullptr;
+    const float *noise = a.noise.data && a.choice ? row_of<float>(a.noise, r) + v0 : nullptr;
+    float add[C][N];
+    if (bias) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int e = (c * Threads + tid) * N;
+            if (e < whole) load_floats(bias, e, add[c]);
+        }
+    }
+    int32_t L = 0;
+    if (History) {
+        constexpr int Held = Threads == 64 ? 8 : 4;
+        int32_t id[Held];
+        float held[Held];
         const uint32_t hrow = row_index(a.history, r);
+        load_history<Threads, Held>(a.history, hrow, id);
+        L = live_history(a, r);
         const RowRates rate = rates_of(a, r);
 #pragma unroll
         for (int i = 0; i < Tile; i += 4 * Threads)
             *reinterpret_cast<u32x4 *>(&s_seen[i + 4 * tid]) = u32x4{kUnseen, kUnseen, kUnseen, kUnseen};
         __syncthreads();
-        uint64_t mine = 0;      // which of this thread's ids it counted first
-        int k = 0;
-        for (int32_t i = tid; i < L; i += Threads, ++k) {
-            const int32_t id = load_id(a.history, hrow, i, a.vocab) - v0;
-            if (id >= 0 && id < n && atomicAdd(&s_seen[id], 1u) == kUnseen && k < 64) mine |= uint64_t(1) << k;
-        }
-        __syncthreads();
-        if (L <= 64 * Threads) {
-            for (; mine; mine &= mine - 1) {
-                const int32_t id = load_id(a.history, hrow, tid + __builtin_ctzll(mine) * Threads, a.vocab) - v0;
-                s_seen[id] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[id]), s_seen[id] + 1));
+        if (L > 0) {
+#pragma unroll
+            for (int h = 0; h < Held; ++h) {
+                id[h] = tid + h * Threads < L && id[h] >= v0 && id[h] - v0 < n ? id[h] - v0 : -1;
+                if (id[h] >= 0) held[h] = static_cast<float>(logits[id[h]]);
             }
-        } else {
-            for (int e = tid; e < n; e += Threads)
-                if (s_seen[e] != kUnseen)
+#pragma unroll
+            for (int h = 0; h < Held; ++h)
+                if (id[h] >= 0 && atomicAdd(&s_seen[id[h]], 1u) != kUnseen) id[h] = -1;    // another's
+            uint64_t mine = 0;      // of the ids beyond those held, which this thread counted first
+            int k = 0;
+            for (int32_t i = tid + Held * Threads; i < L; i += Threads, ++k) {
+                const int32_t e = load_id(a.history, hrow, i, a.vocab) - v0;
+                if (e >= 0 && e < n && atomicAdd(&s_seen[e], 1u) == kUnseen && k < 64) mine |= uint64_t(1) << k;
+            }
+            __syncthreads();
+            if (L <= (Held + 64) * Threads) {
+#pragma unroll
+                for (int h = 0; h < Held; ++h)
+                    if (id[h] >= 0) s_seen[id[h]] = __float_as_uint(penalise(a, rate, held[h], s_seen[id[h]] + 1));
+                for (; mine; mine &= mine - 1) {
+                    const int32_t i = tid + (Held + __builtin_ctzll(mine)) * Threads;
+                    const int32_t e = load_id(a.history, hrow, i, a.vocab) - v0;
                     s_seen[e] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
+                }
+            } else {
+                for (int e = tid; e < n; e += Threads)
+                    if (s_seen[e] != kUnseen)
+                        s_seen[e] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
-    const float *bias = a.bias.data ? row_of<float>(a.bias, r) + v0 : nullptr;
-    const float *noise = a.noise.data && a.choice ? row_of<float>(a.noise, r) + v0 : nullptr;
     O *out = reinterpret_cast<O *>(a.out) + static_cast<int64_t>(r) * a.out_stride + v0;
     Best best = {-INFINITY, INT32_MAX};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int e = (c * Threads + tid) * N;
         if (e < whole) {
-            float x[N], f[N], g[N];
-            if (bias) load_floats(bias, e, f);
+            float x[N], g[N];
             if (noise) load_floats(noise, e, g);
             for (int j = 0; j < N; ++j) x[j] = entry<T>(raw[c], j);
             if (History && L > 0) {
@@ -167,7 +216,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
                 }
             }
             if (bias)
-                for (int j = 0; j < N; ++j) x[j] = x[j] + f[j];
+                for (int j = 0; j < N; ++j) x[j] = x[j] + add[c][j];
             if (a.inv_temperature.data)
                 for (int j = 0; j < N; ++j) x[j] = x[j] * inv_t;
             if (mask) mask_entries(x, chunk_bits<T>(bytes[c]));
@@ -295,11 +344,12 @@ __global__ void __launch_bounds__(kThreads) adjust_group_kernel(GroupArgs g, int
 }
 
 // The choice of rows of several tiles, a workgroup per row.
-__global__ void __launch_bounds__(kThreads) choose_kernel(AdjustArgs a, int64_t first, int32_t tiles, const Best *parts) {
+template <int Threads>
+__global__ void __launch_bounds__(Threads) choose_kernel(AdjustArgs a, int64_t first, int32_t tiles, const Best *parts) {
     const uint32_t r = static_cast<uint32_t>(first + blockIdx.x);
     Best best = {-INFINITY, INT32_MAX};
-    for (int32_t t = threadIdx.x; t < tiles; t += kThreads) best = better(best, parts[static_cast<int64_t>(r) * tiles + t]);
-    best = block_best<kThreads>(best);
+    for (int32_t t = threadIdx.x; t < tiles; t += Threads) best = better(best, parts[static_cast<int64_t>(r) * tiles + t]);
+    best = block_best<Threads>(best);
     if (threadIdx.x == 0) store_choice(a, r, best);
 }
 
@@ -354,7 +404,8 @@ struct AdjustLaunch {
         });
         if (a.choice && n > 1)
             in_launches(a.rows, [&](int64_t first, unsigned count) {
-                hipLaunchKernelGGL(choose_kernel, dim3(count), dim3(kThreads), 0, st, a, first, n, parts);
+                if (n <= 256) hipLaunchKernelGGL((choose_kernel<64>), dim3(count), dim3(64), 0, st, a, first, n, parts);
+                else hipLaunchKernelGGL((choose_kernel<256>), dim3(count), dim3(256), 0, st, a, first, n, parts);
             });
     }
 
