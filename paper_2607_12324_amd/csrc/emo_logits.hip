@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
     }
     int32_t L = 0;
     if (History) {
-        constexpr int Held = Threads == 64 ? 8 : 4;
+        constexpr int Held = Threads == 64 ? 8 : 4;     // ids a thread takes in the first round trip
         int32_t id[Held];
         float held[Held];
         const uint32_t hrow = row_index(a.history, r);
@@ -372,22 +372,14 @@ bool small_rows(const AdjustArgs &a, GroupArgs *g) {
            narrow(a.mask, &g->mask) && narrow(a.noise, &g->noise);
 }
 
-// A row's tiles: of 8,192 entries for workgroups of 256 threads while that gives work to every compute
-// unit (4 workgroups each), of 2,048 for single waves on shorter rows and for few rows.
-// Rows that a group of lanes takes: of at most 64 entries, with a history of at most 64 ids (each is
-// compared with every entry; longer ones are counted in LDS).
-bool small_rows(const AdjustArgs &a) { return a.vocab <= 64 && (!a.history.data || a.history.cols <= 64); }
+// A row's tiles: one of 2,048 entries by a wave; longer rows of 4,096 by 256 threads (2 x 2^20 entries: 5.7 us,
+// tiles of 2,048 by single waves 7.7).  Every tile looks through its row's whole history: a long one wants
+// fewer, 8,192 entries by 512 threads, where that leaves 4 workgroups a compute unit (333 x 100,003 with up
+// to 4,096 ids: 71 us against 85; with 1,024 ids both take the same, with few the smaller tiles less).
+constexpr int kWaveTile = 2048, kTile = 4096, kLongTile = 8192;
+constexpr int kLongHistory = 2048;
 
-struct Tiling {
-    int threads;
-    int64_t tiles;
-};
-
-Tiling tiling(int64_t rows, int64_t vocab) {
-    const int64_t wide = (vocab + 8191) / 8192;
-    if (vocab > 2048 && rows * wide >= 1024) return {512, wide};
-    return {64, (vocab + 2047) / 2048};
-}
+int64_t tiles_of(int64_t vocab, int tile) { return (vocab + tile - 1) / tile; }
 
 struct AdjustLaunch {
     const AdjustArgs &a;
@@ -395,7 +387,8 @@ struct AdjustLaunch {
     hipStream_t st;
 
     template <typename T, typename O, int Threads, int PerThread>
-    void tiles(int32_t n) const {
+    void tiles() const {
+        const int32_t n = static_cast<int32_t>(tiles_of(a.vocab, Threads * PerThread));
         in_pieces(a.rows, n, [&](uint32_t first, unsigned count, const Pieces &pieces) {
             if (a.history.data)
                 hipLaunchKernelGGL((adjust_tile_kernel<T, O, Threads, PerThread, true>), dim3(count), dim3(Threads), 0, st, a, first, pieces, parts);
@@ -422,16 +415,15 @@ struct AdjustLaunch {
             });
             return;
         }
-        const Tiling t = tiling(a.rows, a.vocab);
-        if (t.threads == 64) tiles<T, O, 64, 32>(static_cast<int32_t>(t.tiles));
-        else tiles<T, O, 512, 16>(static_cast<int32_t>(t.tiles));
+        if (a.vocab <= kWaveTile) tiles<T, O, 64, 32>();
+        else if (a.history.data && a.history.cols > kLongHistory && a.rows * tiles_of(a.vocab, kLongTile) >= 1024) tiles<T, O, 512, 16>();
+        else tiles<T, O, 256, 16>();
     }
 };
 
-// Workspace bytes of a call: the best entry of every tile of rows of several.
+// Workspace bytes of a call: the best entry of every tile of rows of several (with the smaller tiles).
 int64_t adjust_bytes(int64_t rows, int64_t vocab) {
-    const int64_t tiles = tiling(rows, vocab).tiles;
-    return tiles > 1 ? rows * tiles * static_cast<int64_t>(sizeof(Best)) : 0;
+    return vocab <= kTile ? 0 : rows * tiles_of(vocab, kTile) * static_cast<int64_t>(sizeof(Best));
 }
 
 }  // namespace
