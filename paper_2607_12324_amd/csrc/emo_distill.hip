@@ -185,7 +185,7 @@ __device__ __forceinline__ Running block_stats(const Running &run, float log2e_t
 // than a chunk) an entry a lane.  Masked entries are -infinity.
 template <typename T, int Threads, int C>
 struct Piece {
-    static constexpr bool Early = C <= 8;       // longer rows have no registers to hold the mask's bytes meanwhile
+    static constexpr bool Early = C <= 8;       // longer rows have no registers to hold the mask's bytes meanwhile: LDS does
     u32x4 raw[C];
     uint32_t bytes[C];
     float x;            // this lane's entry of the rest, or -infinity
@@ -198,10 +198,10 @@ struct Piece {
         if (Early && mask) load_mask<T, Threads, C>(mask, whole, bytes);
     }
 
-    // `n` as in load.
-    __device__ __forceinline__ void apply(const uint32_t *mask, int32_t n) {
+    // `n` as in load; `staged`: the mask's words in LDS, where the bytes were not loaded.
+    __device__ __forceinline__ void apply(const uint32_t *mask, const uint32_t *staged, int32_t n) {
         if (!mask) return;
-        if (!Early) load_mask<T, Threads, C>(mask, n / kChunk<T> * kChunk<T>, bytes);
+        if (!Early) load_mask<T, Threads, C>(staged, n / kChunk<T> * kChunk<T>, bytes);
 #pragma unroll
         for (int c = 0; c < C; ++c) mask_chunk<T>(raw[c], chunk_bits<T>(bytes[c]));
     }
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(Threads) forward_kernel(DistillArgs a, uint32_
     for (int32_t at = 0; at < n; at += Step) {
         now = next;
         if (n - at > Step) next.load(logits + at + Step, mask ? mask + (at + Step) / 32 : nullptr, min(n - at - Step, Step));
-        now.apply(mask, min(n - at, Step));
+        now.apply(mask, nullptr, min(n - at, Step));
         add_entries<T, C>(run, now.raw, now.x, a.log2e_tau);
     }
     run = block_stats<Threads>(run, a.log2e_tau, s_red);
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(Threads) backward_kernel(DistillArgs a, uint32
     const float *st = row_of<float>(a.stats, r);
     const float m = st[0], s = st[1];
     const float rate = row_value(a.scale, r, 1.f) * a.tau;
-    piece.apply(mask, n);
+    piece.apply(mask, nullptr, n);
     __syncthreads();
     sum_equal_ids<Threads>(t, a.entries, v0, hi);
     O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride + v0;
@@ -344,15 +344,31 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     const uint32_t r = static_cast<uint32_t>(first + blockIdx.x);
     const T *logits = row_of<T>(a.logits, r);
     const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
-    Piece<T, Threads, C> piece;
+    using Held = Piece<T, Threads, C>;
+    Held piece;
+    constexpr int Words = Held::Early ? 1 : PerThread / 32;
+    __shared__ uint32_t s_mask[Held::Early ? 1 : Words * Threads];
+    uint32_t words[Words];
+    const int32_t all_words = (a.vocab + 31) / 32;
+    if (!Held::Early && mask) {
+#pragma unroll
+        for (int i = 0; i < Words; ++i)
+            if (tid + i * Threads < all_words) words[i] = mask[tid + i * Threads];
+    }
     piece.load(logits, mask, a.vocab);
+    if (!Held::Early && mask) {
+#pragma unroll
+        for (int i = 0; i < Words; ++i)
+            if (tid + i * Threads < all_words) s_mask[tid + i * Threads] = words[i];
+    }
     const Teacher t = teacher_in(lds, a.entries);
     if (tid < 64) {
         const bool has = load_teacher(a, r, logits, mask, 0, a.vocab, t);
         if (tid == 0) s_has = has;
     }
     const float rate = row_value(a.scale, r, 1.f) * a.tau;
-    piece.apply(mask, a.vocab);
+    if (!Held::Early && mask) __syncthreads();
+    piece.apply(mask, s_mask, a.vocab);
     Running run;
     add_entries<T, C>(run, piece.raw, piece.x, a.log2e_tau);
     __syncthreads();

@@ -97,13 +97,13 @@ __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r)
 
 constexpr uint32_t kUnseen = 0xffffffffu;
 
-// The first Held * Threads ids of a row's history, as they stand (ids of 64 bits cut to -1 where they do not
-// fit 32); -1 from `cols` on.
+// Ids `from` to from + Held * Threads of a row's history, as they stand, all in flight together (ids of 64 bits
+// that do not fit 32 as -1; the last one again from `cols` on).
 template <int Threads, int Held>
-__device__ __forceinline__ void load_history(const Mat &m, uint32_t row, int32_t (&id)[Held]) {
-    const int tid = threadIdx.x;
+__device__ __forceinline__ void load_history(const Mat &m, uint32_t row, int32_t from, int32_t (&id)[Held]) {
     const int64_t base = static_cast<int64_t>(row) * m.row_stride;
-    const auto at = [&](int h) { return base + static_cast<int64_t>(min(tid + h * Threads, m.cols - 1)) * m.col_stride; };
+    const int32_t first = from + static_cast<int32_t>(threadIdx.x);
+    const auto at = [&](int h) { return base + static_cast<int64_t>(min(first + h * Threads, m.cols - 1)) * m.col_stride; };
     if (m.dtype == EMO_U8) {
 #pragma unroll
         for (int h = 0; h < Held; ++h) id[h] = reinterpret_cast<const uint8_t *>(m.data)[at(h)];
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
         int32_t id[Held];
         float held[Held];
         const uint32_t hrow = row_index(a.history, r);
-        load_history<Threads, Held>(a.history, hrow, id);
+        load_history<Threads, Held>(a.history, hrow, 0, id);
         L = live_history(a, r);
         const RowRates rate = rates_of(a, r);
 #pragma unroll
@@ -177,10 +177,14 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
             for (int h = 0; h < Held; ++h)
                 if (id[h] >= 0 && atomicAdd(&s_seen[id[h]], 1u) != kUnseen) id[h] = -1;    // another's
             uint64_t mine = 0;      // of the ids beyond those held, which this thread counted first
-            int k = 0;
-            for (int32_t i = tid + Held * Threads; i < L; i += Threads, ++k) {
-                const int32_t e = load_id(a.history, hrow, i, a.vocab) - v0;
-                if (e >= 0 && e < n && atomicAdd(&s_seen[e], 1u) == kUnseen && k < 64) mine |= uint64_t(1) << k;
+            for (int32_t from = Held * Threads, k = 0; from < L; from += Held * Threads, k += Held) {
+                int32_t more[Held];
+                load_history<Threads, Held>(a.history, hrow, from, more);
+#pragma unroll
+                for (int h = 0; h < Held; ++h) {
+                    const int32_t e = more[h] >= v0 ? more[h] - v0 : n;
+                    if (from + tid + h * Threads < L && e < n && atomicAdd(&s_seen[e], 1u) == kUnseen && k < 64) mine |= uint64_t(1) << (k + h);
+                }
             }
             __syncthreads();
             if (L <= (Held + 64) * Threads) {
@@ -377,7 +381,7 @@ bool small_rows(const AdjustArgs &a, GroupArgs *g) {
 // fewer, 8,192 entries by 512 threads, where that leaves 4 workgroups a compute unit (333 x 100,003 with up
 // to 4,096 ids: 71 us against 85; with 1,024 ids both take the same, with few the smaller tiles less).
 constexpr int kWaveTile = 2048, kTile = 4096, kLongTile = 8192;
-constexpr int kLongHistory = 2048;
+constexpr int kShortHistory = 512, kLongHistory = 2048;      // a wave takes 512 ids at once
 
 int64_t tiles_of(int64_t vocab, int tile) { return (vocab + tile - 1) / tile; }
 
@@ -415,8 +419,10 @@ struct AdjustLaunch {
             });
             return;
         }
-        if (a.vocab <= kWaveTile) tiles<T, O, 64, 32>();
-        else if (a.history.data && a.history.cols > kLongHistory && a.rows * tiles_of(a.vocab, kLongTile) >= 1024) tiles<T, O, 512, 16>();
+        const int32_t ids = a.history.data ? a.history.cols : 0;
+        const int64_t wide = tiles_of(a.vocab, kLongTile);
+        if (a.vocab <= kWaveTile && ids <= kShortHistory) tiles<T, O, 64, 32>();
+        else if (ids > kLongHistory && (wide == 1 || a.rows * wide >= 1024)) tiles<T, O, 512, 16>();
         else tiles<T, O, 256, 16>();
     }
 };

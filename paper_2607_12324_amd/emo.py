@@ -125,7 +125,7 @@ lib = _load_library()
 
 
 def _check(status: int):
-    if status != OK:
+    if status:
         raise EmoError(status, lib.emo_last_error().decode())
 
 
@@ -460,23 +460,17 @@ def _logits_shape(logits):
     return shape[0], shape[1], logits.get_device()
 
 
-def _placed(call):
-    """Makes the logits' device and the given stream current for a call on logits.  Tensors that the call
-    makes (outputs, workspace) then belong to its stream: a captured call owns its workspace, and a
-    reused one is free of the calls before it."""
-    @functools.wraps(call)
-    def placed(logits, *args, stream=None, **kw):
-        _, _, index = _logits_shape(logits)
-        if stream is not None:
-            if stream.device != logits.device:
-                raise ValueError(f"the stream is on {stream.device}, the logits are on {logits.device}")
-            with _torch.cuda.stream(stream):
-                return call(logits, *args, **kw)
-        if index != _device():
-            with _torch.cuda.device(index):
-                return call(logits, *args, **kw)
+def _elsewhere(call, logits, stream, *args, **kw):
+    """The call with the logits' device and the given stream made current.  Tensors that it makes
+    (outputs, workspace) then belong to its stream: a captured call owns its workspace, and a reused one
+    is free of the calls before it."""
+    if stream is None:
+        with _torch.cuda.device(logits.device):
+            return call(logits, *args, **kw)
+    if stream.device != logits.device:
+        raise ValueError(f"the stream is on {stream.device}, the logits are on {logits.device}")
+    with _torch.cuda.stream(stream):
         return call(logits, *args, **kw)
-    return placed
 
 
 def _workspace(given, size_call, rows: int, vocab: int, logits):
@@ -494,10 +488,9 @@ def _workspace(given, size_call, rows: int, vocab: int, logits):
     return given.data_ptr(), given.numel() * given.element_size(), given
 
 
-@_placed
 def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None, repetition=None,
                   frequency=None, presence=None, bias=None, inv_temperature=None, mask=None, noise=None,
-                  out=None, choice=None, workspace=None):
+                  out=None, choice=None, workspace=None, stream=None):
     """Penalties, bias, temperature and mask on rows of logits, and a choice from them
     (emo_adjust_logits).  Returns (out, choice): what was given; the adjusted logits are allocated
     (in the logits' type) when neither is.
@@ -507,6 +500,10 @@ def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None
     [rows] uint8, int32 or int64.  Row r reads row r % n of each; rows defaults to the logits' n.
     `stream`: the stream to run on (default: the current one of the logits' device)."""
     n, V, index = _logits_shape(logits)
+    if stream is not None or index != _device():
+        return _elsewhere(adjust_logits, logits, stream, rows, history=history, lengths=lengths, repetition=repetition,
+                          frequency=frequency, presence=presence, bias=bias, inv_temperature=inv_temperature, mask=mask,
+                          noise=noise, out=out, choice=choice, workspace=workspace)
     if rows is None:
         rows = n
     if out is None and choice is None:
@@ -529,14 +526,16 @@ def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None
     return out, choice
 
 
-@_placed
 def distill_forward(logits, ids, teacher, temperature: float = 1.0, *, mask=None, loss=None, stats=None,
-                    workspace=None):
+                    workspace=None, stream=None):
     """Cross entropy of the logits [N, V] against a teacher's top entries (emo_distill_forward):
     ids [n, K], teacher [n, K] or one row each.  Returns (loss [N], stats [N, 2] for the backward
     pass), allocated when not given.  Autograd does not see it: distill_backward is the gradient.
     `stream` as in adjust_logits."""
     N, V, index = _logits_shape(logits)
+    if stream is not None or index != _device():
+        return _elsewhere(distill_forward, logits, stream, ids, teacher, temperature, mask=mask, loss=loss, stats=stats,
+                          workspace=workspace)
     loss = _torch.empty(N, dtype=_torch.float32, device=logits.device) if loss is None else loss
     stats = _torch.empty((N, 2), dtype=_torch.float32, device=logits.device) if stats is None else stats
     ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, logits)
@@ -547,12 +546,14 @@ def distill_forward(logits, ids, teacher, temperature: float = 1.0, *, mask=None
     return loss, stats
 
 
-@_placed
-def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, grad=None):
+def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, grad=None,
+                     stream=None):
     """Gradient [N, V] of sum(scale * loss) by the logits, from the statistics that distill_forward
     returned for the same operands (emo_distill_backward); scale [n] or None (1).  `grad` may be the
     logits.  `stream` as in adjust_logits."""
     N, V, index = _logits_shape(logits)
+    if stream is not None or index != _device():
+        return _elsewhere(distill_backward, logits, stream, stats, ids, teacher, temperature, scale=scale, mask=mask, grad=grad)
     grad = _torch.empty((N, V), dtype=logits.dtype, device=logits.device) if grad is None else grad
     _check(lib.emo_distill_backward(
         N, V, _operand(logits, "logits", index), _operand(stats, "stats", index), _operand(ids, "ids", index),
@@ -561,12 +562,14 @@ def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, s
     return grad
 
 
-@_placed
 def distill_step(logits, ids, teacher, temperature: float = 1.0, *, scale=None, mask=None, loss=None, grad=None,
-                 workspace=None):
+                 workspace=None, stream=None):
     """Loss [N] and gradient [N, V] in one call (emo_distill_step), for a scale known beforehand (e.g.
     [1 / N]).  `grad` may be the logits.  `stream` as in adjust_logits."""
     N, V, index = _logits_shape(logits)
+    if stream is not None or index != _device():
+        return _elsewhere(distill_step, logits, stream, ids, teacher, temperature, scale=scale, mask=mask, loss=loss, grad=grad,
+                          workspace=workspace)
     loss = _torch.empty(N, dtype=_torch.float32, device=logits.device) if loss is None else loss
     grad = _torch.empty((N, V), dtype=logits.dtype, device=logits.device) if grad is None else grad
     ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, logits)
