@@ -66,14 +66,30 @@ __device__ __forceinline__ bool load_teacher(const DistillArgs &a, uint32_t r, c
     const int K = a.entries, lane = threadIdx.x % 64;
     const uint32_t irow = row_index(a.ids, r), trow = row_index(a.teacher, r);
     float tm = -INFINITY;
-    for (int k = lane; k < K; k += 64) {
-        int32_t id = load_id(a.ids, irow, k, a.vocab);
-        const float v = load_float(a.teacher, trow, k);
-        if (id >= 0 && (v == -INFINITY || !allowed(mask, id))) id = -1;
-        t.id[k] = id;
-        t.p[k] = v;
-        if (id >= lo && id < hi) t.x[k] = static_cast<float>(logits[id]);
-        if (id >= 0) tm = fmaxf(tm, fmaxf(v, -3.4028235e38f));      // a NaN that counts is no -infinity
+    constexpr int Held = 2;     // 128 entries a round trip
+    for (int from = 0; from < K; from += 64 * Held) {
+        int32_t id[Held];
+        float v[Held], x[Held];
+        uint32_t open[Held];
+        load_ids<64, Held>(a.ids, irow, from, id);
+        load_values<64, Held>(a.teacher, trow, from, v);
+#pragma unroll
+        for (int h = 0; h < Held; ++h) {
+            const bool counts = id[h] >= 0 && id[h] < a.vocab;
+            open[h] = counts ? 1u : 0u;
+            if (counts && mask) open[h] = mask[id[h] >> 5] >> (id[h] & 31);
+            if (id[h] >= lo && id[h] < hi) x[h] = static_cast<float>(logits[id[h]]);
+        }
+#pragma unroll
+        for (int h = 0; h < Held; ++h) {
+            const int k = from + h * 64 + lane;
+            if (k >= K) continue;
+            if (v[h] == -INFINITY || !(open[h] & 1u)) id[h] = -1;
+            t.id[k] = id[h];
+            t.p[k] = v[h];
+            t.x[k] = x[h];
+            if (id[h] >= 0) tm = fmaxf(tm, fmaxf(v[h], -3.4028235e38f));      // a NaN that counts is no -infinity
+        }
     }
     for (int k = K + lane; k < (K + 3) / 4 * 4; k += 64) t.id[k] = -1;
     tm = wave_max(tm);
@@ -182,8 +198,9 @@ __device__ __forceinline__ Running block_stats(const Running &run, float log2e_t
 }
 
 // What a workgroup holds of a row: n entries from v0 on, those of whole chunks 16 bytes a lane, the rest (fewer
-// than a chunk) an entry a lane.  Masked entries are -infinity.
-template <typename T, int Threads, int C>
+// than a chunk) an entry a lane.  Masked entries are -infinity.  Once: the logits are not read again (forward
+// 2,048 x 131,072 bf16: 99 us against 104 without the hint; backward 199 with it against 187).
+template <typename T, int Threads, int C, bool Once>
 struct Piece {
     static constexpr bool Early = C <= 8;       // longer rows have no registers to hold the mask's bytes meanwhile: LDS does
     u32x4 raw[C];
@@ -192,7 +209,7 @@ struct Piece {
 
     __device__ __forceinline__ void load(const T *logits, const uint32_t *mask, int32_t n) {
         const int32_t whole = n / kChunk<T> * kChunk<T>, e = whole + static_cast<int32_t>(threadIdx.x);
-        load_chunks<T, Threads, C>(logits, whole, raw);
+        load_chunks<T, Threads, C, Once>(logits, whole, raw);
         x = -INFINITY;
         if (e < n && allowed(mask, e)) x = static_cast<float>(logits[e]);
         if (Early && mask) load_mask<T, Threads, C>(mask, whole, bytes);
@@ -223,7 +240,7 @@ __global__ void __launch_bounds__(Threads) forward_kernel(DistillArgs a, uint32_
     const T *logits = row + v0;
     const uint32_t *row_mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
     const uint32_t *mask = row_mask ? row_mask + v0 / 32 : nullptr;
-    Piece<T, Threads, C> now, next;
+    Piece<T, Threads, C, true> now, next;
     next.load(logits, mask, min(n, Step));
     const Teacher t = teacher_in(lds, a.entries);
     bool has = false;
@@ -271,8 +288,8 @@ __global__ void __launch_bounds__(64) finish_kernel(DistillArgs a, int64_t first
 
 // Writes the gradient of a workgroup's piece (n entries from v0 of the row on), and over it that of the
 // teacher's entries.  rate = scale * temperature.
-template <typename T, typename O, int Threads, int C>
-__device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece<T, Threads, C> &piece, const uint32_t *mask, O *grad,
+template <typename T, typename O, int Threads, int C, bool Once>
+__device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece<T, Threads, C, Once> &piece, const uint32_t *mask, O *grad,
                                                int32_t v0, int32_t n, bool has, float m, float s, float rate, const Teacher &t) {
     constexpr int N = kChunk<T>;
     const int tid = threadIdx.x;
@@ -288,7 +305,7 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece
             for (int j = 0; j < N; ++j) g[j] = has ? share * exp2_fast((entry<T>(piece.raw[c], j) - m) * a.log2e_tau) : 0.f;
             if (odd)
                 for (int j = 0; j < N; ++j) g[j] = allowed(mask, e + j) ? g[j] : 0.f;
-            store_chunk(grad, e, g);
+            store_chunk<true>(grad, e, g);
         }
     }
     if (whole + tid < n) {
@@ -315,7 +332,7 @@ __global__ void __launch_bounds__(Threads) backward_kernel(DistillArgs a, uint32
     const T *row = row_of<T>(a.logits, r);
     const uint32_t *row_mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
     const uint32_t *mask = row_mask ? row_mask + v0 / 32 : nullptr;
-    Piece<T, Threads, C> piece;
+    Piece<T, Threads, C, false> piece;
     piece.load(row + v0, mask, n);
     const Teacher t = teacher_in(lds, a.entries);
     const int64_t hi = static_cast<int64_t>(v0) + n;
@@ -344,41 +361,44 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     const uint32_t r = static_cast<uint32_t>(first + blockIdx.x);
     const T *logits = row_of<T>(a.logits, r);
     const uint32_t *mask = a.mask.data ? row_of<uint32_t>(a.mask, r) : nullptr;
-    using Held = Piece<T, Threads, C>;
-    Held piece;
-    constexpr int Words = Held::Early ? 1 : PerThread / 32;
-    __shared__ uint32_t s_mask[Held::Early ? 1 : Words * Threads];
-    uint32_t words[Words];
-    const int32_t all_words = (a.vocab + 31) / 32;
-    if (!Held::Early && mask) {
-#pragma unroll
-        for (int i = 0; i < Words; ++i)
-            if (tid + i * Threads < all_words) words[i] = mask[tid + i * Threads];
-    }
-    piece.load(logits, mask, a.vocab);
-    if (!Held::Early && mask) {
-#pragma unroll
-        for (int i = 0; i < Words; ++i)
-            if (tid + i * Threads < all_words) s_mask[tid + i * Threads] = words[i];
-    }
+    // The teacher first, by one wave: loads return in order, so behind the row's it would wait for all of them.
+    // The other waves' rows are on their way meanwhile, and still while equal ids are summed.
     const Teacher t = teacher_in(lds, a.entries);
     if (tid < 64) {
         const bool has = load_teacher(a, r, logits, mask, 0, a.vocab, t);
         if (tid == 0) s_has = has;
+        asm volatile("" ::: "memory");
+    }
+    using Held = Piece<T, Threads, C, true>;
+    Held piece;
+    constexpr int Words = Held::Early ? 1 : PerThread / 32;
+    __shared__ uint32_t s_mask[Held::Early ? 1 : Words * Threads];
+    const int32_t all_words = (a.vocab + 31) / 32;
+    if (!Held::Early && mask) {
+        uint32_t words[Words];
+#pragma unroll
+        for (int i = 0; i < Words; ++i)
+            if (tid + i * Threads < all_words) words[i] = mask[tid + i * Threads];
+        piece.load(logits, mask, a.vocab);
+#pragma unroll
+        for (int i = 0; i < Words; ++i)
+            if (tid + i * Threads < all_words) s_mask[tid + i * Threads] = words[i];
+    } else {
+        piece.load(logits, mask, a.vocab);
     }
     const float rate = row_value(a.scale, r, 1.f) * a.tau;
-    if (!Held::Early && mask) __syncthreads();
+    __syncthreads();
+    sum_equal_ids<Threads>(t, a.entries, 0, a.vocab);
     piece.apply(mask, s_mask, a.vocab);
     Running run;
     add_entries<T, C>(run, piece.raw, piece.x, a.log2e_tau);
-    __syncthreads();
-    sum_equal_ids<Threads>(t, a.entries, 0, a.vocab);
     run = block_stats<Threads>(run, a.log2e_tau, s_red);
     const bool has = s_has != 0;
     if (a.loss && tid < 64) {
         const float loss = has ? teacher_loss(a, t, run.m, run.s) : 0.f;
         if (tid == 0) store_loss(a, r, loss);
     }
+    anew(piece.raw);
     O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride;
     write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t);
 }

@@ -97,28 +97,6 @@ __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r)
 
 constexpr uint32_t kUnseen = 0xffffffffu;
 
-// Ids `from` to from + Held * Threads of a row's history, as they stand, all in flight together (ids of 64 bits
-// that do not fit 32 as -1; the last one again from `cols` on).
-template <int Threads, int Held>
-__device__ __forceinline__ void load_history(const Mat &m, uint32_t row, int32_t from, int32_t (&id)[Held]) {
-    const int64_t base = static_cast<int64_t>(row) * m.row_stride;
-    const int32_t first = from + static_cast<int32_t>(threadIdx.x);
-    const auto at = [&](int h) { return base + static_cast<int64_t>(min(first + h * Threads, m.cols - 1)) * m.col_stride; };
-    if (m.dtype == EMO_U8) {
-#pragma unroll
-        for (int h = 0; h < Held; ++h) id[h] = reinterpret_cast<const uint8_t *>(m.data)[at(h)];
-    } else if (m.dtype == EMO_I32) {
-#pragma unroll
-        for (int h = 0; h < Held; ++h) id[h] = reinterpret_cast<const int32_t *>(m.data)[at(h)];
-    } else {
-        int64_t wide[Held];
-#pragma unroll
-        for (int h = 0; h < Held; ++h) wide[h] = reinterpret_cast<const int64_t *>(m.data)[at(h)];
-#pragma unroll
-        for (int h = 0; h < Held; ++h) id[h] = wide[h] == static_cast<int32_t>(wide[h]) ? static_cast<int32_t>(wide[h]) : -1;
-    }
-}
-
 // A workgroup per tile of Threads * PerThread entries of a row.  Bound by memory and, with a history, by what
 // has to follow each other in a workgroup: so everything that needs nothing is loaded at once (logits, mask,
 // bias, length, the first ids), and one more round trip fetches the logits of the ids in the tile.  The ids
@@ -160,7 +138,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
         int32_t id[Held];
         float held[Held];
         const uint32_t hrow = row_index(a.history, r);
-        load_history<Threads, Held>(a.history, hrow, 0, id);
+        load_ids<Threads, Held>(a.history, hrow, 0, id);
         L = live_history(a, r);
         const RowRates rate = rates_of(a, r);
 #pragma unroll
@@ -179,7 +157,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
             uint64_t mine = 0;      // of the ids beyond those held, which this thread counted first
             for (int32_t from = Held * Threads, k = 0; from < L; from += Held * Threads, k += Held) {
                 int32_t more[Held];
-                load_history<Threads, Held>(a.history, hrow, from, more);
+                load_ids<Threads, Held>(a.history, hrow, from, more);
 #pragma unroll
                 for (int h = 0; h < Held; ++h) {
                     const int32_t e = more[h] >= v0 ? more[h] - v0 : n;
@@ -224,7 +202,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
             if (a.inv_temperature.data)
                 for (int j = 0; j < N; ++j) x[j] = x[j] * inv_t;
             if (mask) mask_entries(x, chunk_bits<T>(bytes[c]));
-            if (a.out) store_chunk(out, e, x);
+            if (a.out) store_chunk<true>(out, e, x);
             if (noise)
                 for (int j = 0; j < N; ++j) x[j] = x[j] + g[j];
             if (a.choice)
@@ -326,7 +304,7 @@ __global__ void __launch_bounds__(kThreads) adjust_group_kernel(GroupArgs g, int
     if (!g.choice) return;
     if (mine && g.noise.data) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_floats(reinterpret_cast<const float *>(row_at(g.noise, r[u])), v, g.vocab, f[u]);
+        for (int u = 0; u < U; ++u) load_floats_once(reinterpret_cast<const float *>(row_at(g.noise, r[u])), v, g.vocab, f[u]);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             for (int j = 0; j < 4; ++j) x[u][j] = x[u][j] + f[u][j];
