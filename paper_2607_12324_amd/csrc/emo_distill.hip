@@ -50,7 +50,8 @@ struct Teacher {
     int32_t *id;
     float *p, *x, *sum;
 };
-constexpr int kTeacherBytes = 16;       // LDS of an entry
+// Floats of LDS that it takes.
+__host__ __device__ constexpr int teacher_floats(int K) { return (K + 3) / 4 * 4 * 4; }
 
 __device__ __forceinline__ Teacher teacher_in(float4 *lds, int K) {
     const int places = (K + 3) / 4 * 4;
@@ -127,6 +128,34 @@ __device__ __forceinline__ void sum_equal_ids(const Teacher &t, int K, int64_t l
             first = first && !(other.w == id && i + 3 < k);
         }
         t.sum[k] = first ? sum : -1.f;
+    }
+}
+
+// A row's probabilities by entry, for the rows a wave takes: a table in LDS of `n` floats and tags to share it
+// out.  64 entries of the list at a time; of those with equal ids (or equal tags) the lowest lane adds to the
+// table, then the next: the list's order, at as many turns as an id stands among the 64.  (Comparing all ids
+// bounded rows of few entries and long lists: 5,985 rows of 86 with 128 entries took 24 us.)
+constexpr int kTags = 256;
+
+__device__ __forceinline__ void gather_probabilities(const Teacher &t, int K, int n, volatile float *table, volatile uint32_t *tags) {
+    const int lane = threadIdx.x % 64;
+    for (int i = lane; i < n; i += 64) table[i] = 0.f;
+    for (int i = lane; i < kTags; i += 64) tags[i] = ~0u;
+    for (int from = 0; from < K; from += 64) {
+        const int32_t id = from + lane < K ? t.id[from + lane] : -1;
+        const float p = id >= 0 ? t.p[from + lane] : 0.f;
+        volatile uint32_t *tag = tags + (id & (kTags - 1));
+        bool pending = id >= 0;
+        while (__any(pending)) {
+            if (pending) {
+                atomicMin(const_cast<uint32_t *>(tag), static_cast<uint32_t>(lane));
+                if (*tag == static_cast<uint32_t>(lane)) {
+                    table[id] = table[id] + p;
+                    *tag = ~0u;
+                    pending = false;
+                }
+            }
+        }
     }
 }
 
@@ -286,11 +315,13 @@ __global__ void __launch_bounds__(64) finish_kernel(DistillArgs a, int64_t first
     }
 }
 
-// Writes the gradient of a workgroup's piece (n entries from v0 of the row on), and over it that of the
-// teacher's entries.  rate = scale * temperature.
+// Writes the gradient of a workgroup's piece (n entries from v0 of the row on).  A wave's row has the teacher's
+// probabilities by entry in `table`; wider ones are written over at the teacher's entries (`sum`).
+// rate = scale * temperature.
 template <typename T, typename O, int Threads, int C, bool Once>
 __device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece<T, Threads, C, Once> &piece, const uint32_t *mask, O *grad,
-                                               int32_t v0, int32_t n, bool has, float m, float s, float rate, const Teacher &t) {
+                                               int32_t v0, int32_t n, bool has, float m, float s, float rate, const Teacher &t,
+                                               const volatile float *table) {
     constexpr int N = kChunk<T>;
     const int tid = threadIdx.x;
     const int32_t whole = n / N * N;
@@ -303,16 +334,19 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece
         if (e < whole) {
             float g[N];
             for (int j = 0; j < N; ++j) g[j] = has ? share * exp2_fast((entry<T>(piece.raw[c], j) - m) * a.log2e_tau) : 0.f;
+            if (Threads == 64 && has)
+                for (int j = 0; j < N; ++j) g[j] = g[j] - rate * table[e + j];
             if (odd)
                 for (int j = 0; j < N; ++j) g[j] = allowed(mask, e + j) ? g[j] : 0.f;
             store_chunk<true>(grad, e, g);
         }
     }
     if (whole + tid < n) {
-        const float g = share * exp2_fast((piece.x - m) * a.log2e_tau);
+        float g = share * exp2_fast((piece.x - m) * a.log2e_tau);
+        if (Threads == 64 && has) g = g - rate * table[whole + tid];
         grad[whole + tid] = static_cast<O>(has && allowed(mask, whole + tid) ? g : 0.f);
     }
-    if (!has) return;
+    if (Threads == 64 || !has) return;
     __syncthreads();        // the entries' own values are in memory before the teacher's go over them
     for (int k = tid; k < a.entries; k += Threads)
         if (!(t.sum[k] < 0.f))
@@ -345,9 +379,11 @@ __global__ void __launch_bounds__(Threads) backward_kernel(DistillArgs a, uint32
     const float rate = row_value(a.scale, r, 1.f) * a.tau;
     piece.apply(mask, nullptr, n);
     __syncthreads();
-    sum_equal_ids<Threads>(t, a.entries, v0, hi);
+    float *table = reinterpret_cast<float *>(lds) + teacher_floats(a.entries);
+    if (Threads == 64) gather_probabilities(t, a.entries, n, table, reinterpret_cast<uint32_t *>(table) + n);
+    else sum_equal_ids<Threads>(t, a.entries, v0, hi);
     O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride + v0;
-    write_gradient(a, piece, mask, grad, v0, n, s_has != 0, m, s, rate, t);
+    write_gradient(a, piece, mask, grad, v0, n, s_has != 0, m, s, rate, t, table);
 }
 
 // Loss and gradient of rows that fit a workgroup's registers: read once, written once.
@@ -388,7 +424,9 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     }
     const float rate = row_value(a.scale, r, 1.f) * a.tau;
     __syncthreads();
-    sum_equal_ids<Threads>(t, a.entries, 0, a.vocab);
+    float *table = reinterpret_cast<float *>(lds) + teacher_floats(a.entries);
+    if (Threads == 64) gather_probabilities(t, a.entries, a.vocab, table, reinterpret_cast<uint32_t *>(table) + a.vocab);
+    else sum_equal_ids<Threads>(t, a.entries, 0, a.vocab);
     piece.apply(mask, s_mask, a.vocab);
     Running run;
     add_entries<T, C>(run, piece.raw, piece.x, a.log2e_tau);
@@ -400,7 +438,7 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     }
     anew(piece.raw);
     O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride;
-    write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t);
+    write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t, table);
 }
 
 // Rows of at most 64 entries: 64 rows a workgroup, in two phases.  The teacher's: a lane per row and a wave per
@@ -698,7 +736,12 @@ void launch_small(const SmallArgs &s, hipStream_t st) {
     });
 }
 
-unsigned teacher_lds(const DistillArgs &a) { return static_cast<unsigned>((a.entries + 3) / 4 * 4 * kTeacherBytes); }
+unsigned teacher_lds(const DistillArgs &a) { return static_cast<unsigned>(teacher_floats(a.entries) * sizeof(float)); }
+
+// With a wave's table of probabilities and its tags.
+unsigned gradient_lds(const DistillArgs &a, int threads) {
+    return teacher_lds(a) + (threads == 64 ? static_cast<unsigned>((a.vocab + kTags) * sizeof(float)) : 0u);
+}
 
 struct ForwardLaunch {
     const DistillArgs &a;
@@ -731,7 +774,7 @@ struct BackwardLaunch {
     void tiles() const {
         const int64_t tiles = (static_cast<int64_t>(a.vocab) + Threads * 32 - 1) / (Threads * 32);
         in_pieces(a.rows, tiles, [&](uint32_t first, unsigned count, const Pieces &pieces) {
-            hipLaunchKernelGGL((backward_kernel<T, O, Threads>), dim3(count), dim3(Threads), teacher_lds(a), st, a, first, pieces);
+            hipLaunchKernelGGL((backward_kernel<T, O, Threads>), dim3(count), dim3(Threads), gradient_lds(a, Threads), st, a, first, pieces);
         });
     }
 
@@ -751,7 +794,7 @@ struct StepLaunch {
     template <typename T, typename O, int Threads, int PerThread>
     void rows() const {
         in_launches(a.rows, [&](int64_t first, unsigned count) {
-            hipLaunchKernelGGL((step_kernel<T, O, Threads, PerThread>), dim3(count), dim3(Threads), teacher_lds(a), st, a, first);
+            hipLaunchKernelGGL((step_kernel<T, O, Threads, PerThread>), dim3(count), dim3(Threads), gradient_lds(a, Threads), st, a, first);
         });
     }
 

@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
     }
     int32_t L = 0;
     if (History) {
-        constexpr int Held = Threads == 64 ? 8 : 4;     // ids a thread takes in the first round trip
+        constexpr int Held = Threads == 64 ? 8 : Threads == 1024 ? 2 : 4;     // ids a thread takes in the first round trip
         int32_t id[Held];
         float held[Held];
         const uint32_t hrow = row_index(a.history, r);
@@ -361,6 +361,12 @@ bool small_rows(const AdjustArgs &a, GroupArgs *g) {
 constexpr int kWaveTile = 2048, kTile = 4096, kLongTile = 8192;
 constexpr int kShortHistory = 512, kLongHistory = 2048;      // a wave takes 512 ids at once
 
+// A choice from few rows of up to 32,768 entries: a workgroup of 1,024 threads per row, which needs neither the
+// second launch nor a workspace (3 us of the calling thread's time each).
+constexpr int kRowTile = 32768;
+
+bool whole_rows(int64_t rows, int64_t vocab) { return vocab > kTile && vocab <= kRowTile && rows <= 256; }
+
 int64_t tiles_of(int64_t vocab, int tile) { return (vocab + tile - 1) / tile; }
 
 struct AdjustLaunch {
@@ -400,6 +406,7 @@ struct AdjustLaunch {
         const int32_t ids = a.history.data ? a.history.cols : 0;
         const int64_t wide = tiles_of(a.vocab, kLongTile);
         if (a.vocab <= kWaveTile && ids <= kShortHistory) tiles<T, O, 64, 32>();
+        else if (a.choice && whole_rows(a.rows, a.vocab)) tiles<T, O, 1024, 32>();
         else if (ids > kLongHistory && (wide == 1 || a.rows * wide >= 1024)) tiles<T, O, 512, 16>();
         else tiles<T, O, 256, 16>();
     }
@@ -407,7 +414,7 @@ struct AdjustLaunch {
 
 // Workspace bytes of a call: the best entry of every tile of rows of several (with the smaller tiles).
 int64_t adjust_bytes(int64_t rows, int64_t vocab) {
-    return vocab <= kTile ? 0 : rows * tiles_of(vocab, kTile) * static_cast<int64_t>(sizeof(Best));
+    return vocab <= kTile || whole_rows(rows, vocab) ? 0 : rows * tiles_of(vocab, kTile) * static_cast<int64_t>(sizeof(Best));
 }
 
 }  // namespace
