@@ -423,7 +423,7 @@ typedef struct {
  *            there is none, which in a byte is 255: a level that emo_evaluate takes for invalid.
  *   rows            0 <= rows < 2^31; vocab: 1 <= V < 2^31.
  *   logits          dense [.][V], EMO_F32, EMO_F16 or EMO_BF16.
- *   history         [.][L] ids, EMO_U8, EMO_I32 or EMO_I64, any strides, 0 <= L < 2^31; ids outside
+ *   history         [.][L] ids, EMO_U8, EMO_I32 or EMO_I64, any strides, 0 <= L <= 2^30; ids outside
  *                   [0, V) are ignored.  lengths: EMO_I32 [.][1] or NULL: only the first lengths[r]
  *                   ids of a row count (clamped to [0, L]).  The three penalties need a history.
  *   repetition, frequency, presence, inv_temperature: EMO_F32 [.][1].
@@ -459,11 +459,11 @@ emo_status emo_adjust_workspace(int64_t rows, int64_t vocab, int64_t *bytes);
  *          scale times the loss's derivative by x_v.
  * The loss is the Kullback-Leibler divergence plus the teacher's entropy, which does not depend on x.
  * A row without a valid entry has loss 0 and gradient 0 whatever its logits are; masked logits are not
- * looked at.  In a row with valid entries a NaN or +infinity among the allowed logits or valid t_k
- * makes the loss NaN, and the gradient wherever the formula does; so do allowed logits that are all
- * -infinity.
+ * looked at.  In a row with valid entries a NaN or +infinity among the allowed logits, or allowed logits
+ * that are all -infinity, make the loss NaN and the gradient NaN at the allowed entries; a NaN or
+ * +infinity among the valid t_k makes the loss NaN and the gradient NaN at the valid ids at least.
  * Sums are held in fp32, in a fixed order: the same call gives the same bits.
- *   rows         0 <= N < 2^31; vocab: 1 <= V < 2^31; temperature finite and > 0.
+ *   rows         0 <= N < 2^31; vocab: 1 <= V < 2^31; 2^-60 <= temperature <= 2^60.
  *   logits       dense [N][V] (all N rows), EMO_F32, EMO_F16 or EMO_BF16.
  *   ids          [.][K], 0 <= K <= 1024, EMO_U8, EMO_I32 or EMO_I64, any strides (level bytes
  *                [K][P] serve as [P][K] with row_stride 1).

@@ -676,9 +676,14 @@ Parts forward_parts(int64_t rows, int64_t vocab) {
     return {static_cast<int32_t>((vocab + span - 1) / span), static_cast<int32_t>(span)};
 }
 
-// Rows that step_kernel holds: up to 131,072 entries of 2 bytes or 65,536 of 4 (half a compute unit's
-// registers); others go by the forward and the backward kernels.
-int64_t resident(int32_t dtype) { return dtype == EMO_F32 ? 65536 : 131072; }
+// Rows that step_kernel takes: up to 131,072 entries of 2 bytes or 65,536 of 4 (half a compute unit's
+// registers); others go by the forward and the backward kernels, and so do few of the widest, which leave
+// most of the card idle (16 x 130,000 bf16: 15 us in three launches, 19 in one; 128 rows: 32 against 24).
+constexpr int64_t kResident = 65536;
+
+bool resident(int64_t rows, int64_t vocab, int32_t dtype) {
+    return vocab <= kResident || (vocab <= 2 * kResident && dtype != EMO_F32 && rows > 32);
+}
 
 int64_t partial_bytes(int64_t rows, int64_t vocab) {
     const Parts p = forward_parts(rows, vocab);
@@ -687,7 +692,7 @@ int64_t partial_bytes(int64_t rows, int64_t vocab) {
 
 // Workspace bytes of a call: the statistics of the rows' parts, and those of the rows of a step in two passes.
 int64_t distill_bytes(int64_t rows, int64_t vocab) {
-    return partial_bytes(rows, vocab) + (vocab > resident(EMO_F32) ? rows * static_cast<int64_t>(sizeof(float2)) : 0);
+    return partial_bytes(rows, vocab) + (vocab > kResident ? rows * static_cast<int64_t>(sizeof(float2)) : 0);
 }
 
 // Bytes from an operand's first row to its last.
@@ -803,6 +808,7 @@ struct StepLaunch {
         SmallArgs small;
         if (small_rows(a, sizeof(O), &small)) return launch_small<T, O, true, true>(small, st);
         if (a.vocab <= 2048) rows<T, O, 64, 32>();
+        else if (a.vocab <= 4096) rows<T, O, 128, 32>();
         else if (a.vocab <= 8192) rows<T, O, 256, 32>();
         else if (a.vocab <= 32768) rows<T, O, 512, 64>();
         else if constexpr (sizeof(T) == 4) rows<T, O, 1024, 64>();
@@ -817,7 +823,9 @@ emo_status distill_operands(Checker &c, DistillArgs &a, int64_t rows, int64_t vo
     emo_status s = check_sizes(rows, vocab);
     if (s != EMO_OK) return s;
     if (!logits || !ids || !teacher) return fail(EMO_ERR_INVALID_ARGUMENT, "logits, ids or teacher is NULL");
-    if (!(temperature > 0.f) || isinf(temperature)) return fail(EMO_ERR_INVALID_ARGUMENT, "temperature must be finite and > 0");
+    // its square and inverse are fp32 numbers with room
+    if (!(temperature >= 0x1p-60f && temperature <= 0x1p60f))
+        return fail(EMO_ERR_INVALID_ARGUMENT, "temperature must be in [2^-60, 2^60]");
     if (ids->cols < 0 || ids->cols > kMaxEntries)
         return fail(EMO_ERR_INVALID_ARGUMENT, "ids has %lld columns, outside [0, %d]", (long long)ids->cols, kMaxEntries);
     a = {};
@@ -911,7 +919,7 @@ emo_status emo_distill_step(int64_t rows, int64_t vocab, const emo_tensor *logit
     a.grad = const_cast<char *>(g.data);
     a.grad_stride = g.row_stride;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (vocab <= resident(a.logits.dtype)) {
+    if (resident(rows, vocab, a.logits.dtype)) {
         by_types(a.logits.dtype, g.dtype, StepLaunch{a, st});
         return launched("emo_distill_step");
     }

@@ -96,6 +96,7 @@ __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r)
 }
 
 constexpr uint32_t kUnseen = 0xffffffffu;
+constexpr int64_t kMaxHistory = int64_t(1) << 30;      // 32 bits hold a place beyond the last id that a thread asks for
 
 // A workgroup per tile of Threads * PerThread entries of a row.  Bound by memory and, with a history, by what
 // has to follow each other in a workgroup: so everything that needs nothing is loaded at once (logits, mask,
@@ -435,6 +436,8 @@ emo_status emo_adjust_logits(int64_t rows, int64_t vocab, const emo_tensor *logi
     if (!logits) return fail(EMO_ERR_INVALID_ARGUMENT, "logits is NULL");
     if (!history && (lengths || repetition || frequency || presence))
         return fail(EMO_ERR_INVALID_ARGUMENT, "lengths and penalties need a history");
+    if (history && history->cols > kMaxHistory)
+        return fail(EMO_ERR_INVALID_ARGUMENT, "history has %lld columns, outside [0, 2^30]", (long long)history->cols);
     if (choice && choice->dtype == EMO_U8 && vocab > 255)
         return fail(EMO_ERR_INVALID_ARGUMENT, "a choice among %lld entries does not fit a byte (255 is none)", (long long)vocab);
     Checker c{rows};

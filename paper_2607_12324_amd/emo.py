@@ -450,13 +450,13 @@ def _logits_shape(logits):
         raise ValueError("logits must be a device tensor")
     if not _DTYPES:
         import torch
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
-                        torch.int64: 5})
         global _torch, _device, _raw_stream
         _torch = torch
         _device = torch._C._cuda_getDevice
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.uint8: 3, torch.int32: 4,
+                        torch.int64: 5})    # last: another thread takes it for the sign that the rest is there
     return shape[0], shape[1], logits.get_device()
 
 

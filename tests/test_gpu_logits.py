@@ -224,6 +224,55 @@ def test_adjust_odd_rates(torch, emo, V):
         assert C.cpu().tolist() == wc.tolist()
 
 
+@pytest.mark.parametrize("V", [2, 7, 40, 61, 75, 2500, 9003, 33001])
+def test_adjust_odd_noise_bias_and_mask_ends(torch, emo, V):
+    """Infinities and NaN in noise and bias; mask bits behind the last entry, which are nobody's."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(size=(4, V)).astype(np.float32)
+    noise, bias = rng.gumbel(size=(4, V)).astype(np.float32), rng.normal(size=(1, V)).astype(np.float32)
+    for a, row in ((noise, 0), (noise, 1), (bias, 0)):
+        a[row][rng.random(V) < 0.2] = [np.nan, -np.inf, np.nan][row]
+    noise[2][rng.random(V) < 0.3] = np.inf
+    noise[3] = np.nan
+    bias[0, V - 1] = -np.inf
+    W = (V + 31) // 32
+    words = orc.mask_words(rng.random((4, V)) < 0.7).copy()
+    if V % 32:
+        words[:, W - 1] |= np.int32(-1) << np.int32(V % 32)
+    for kw in ({"noise": noise}, {"noise": noise, "bias": bias, "mask": words}, {"mask": words}):
+        want, wc = orc.adjust(4, x, **kw)
+        O, C = emo.adjust_logits(dev(torch, x), out=torch.empty((4, V), device="cuda"),
+                                 choice=torch.empty(4, dtype=torch.int64, device="cuda"), **{k: dev(torch, v) for k, v in kw.items()})
+        bits_equal(torch, O, want, "f32", "adjusted")
+        assert C.cpu().tolist() == wc.tolist()
+    i, t = rng.integers(0, V, size=(4, 9)), rng.normal(size=(4, 9)).astype(np.float32)
+    w = orc.distill(x, i, t, 1.0, words)
+    _, tl, tg = bounds(w, V, 9, 1.0, np.ones(4), "f32")
+    loss, g = emo.distill_step(dev(torch, x), dev(torch, i, "i64"), dev(torch, t), mask=dev(torch, words))
+    check_near(loss.cpu().numpy(), w["loss"], tl, "loss")
+    check_near(g.cpu().numpy(), w["grad"], tg, "gradient")
+
+
+def test_distill_teachers_of_nan_and_infinity(torch, emo):
+    """A NaN or an infinity in a teacher's list that counts makes the loss NaN; one at an id that does not, nothing."""
+    for V in (16, 40, 300, 9000):
+        x = np.zeros((5, V), np.float32)
+        i = np.tile(np.arange(4), (5, 1))
+        t = np.zeros((5, 4), np.float32)
+        t[0, 1], t[1, 2], t[2] = np.nan, np.inf, np.nan
+        t[3, 3], i[3, 3] = np.nan, -1
+        X, I, T = dev(torch, x), dev(torch, i, "i32"), dev(torch, t)
+        loss, stats = emo.distill_forward(X, I, T)
+        loss2, g = emo.distill_step(X, I, T)
+        g3 = emo.distill_backward(X, stats, I, T)
+        for a in (loss, loss2):
+            a = a.cpu().numpy()
+            assert np.isnan(a[:3]).all() and abs(a[3:] - np.log(V)).max() < 1e-5
+        for b in (g, g3):
+            b = b.cpu().numpy()
+            assert np.isnan(b[:3, 1]).all() and np.isfinite(b[3:]).all()
+
+
 def test_adjust_masks_that_leave_little(torch, emo):
     """Nothing, only -inf, only the lowest value, only NaN; a byte choice without an entry is 255."""
     for V in (5, 70, 5000):

@@ -89,6 +89,7 @@ def test_adjust_refuses(emo, mem):
     bad(["history"], frequency=mem(R, 1))
     bad(["history"], presence=mem(R, 1))
     bad(["history", "type"], history=mem(R, 9))
+    bad(["history", "columns"], history=mem(1, (1 << 30) + 1, I32, row_stride=0, col_stride=0, data=1 << 33))
     bad(["lengths", "type"], history=mem(R, 9, I32), lengths=mem(R, 1, I64))
     bad(["presence", "columns"], history=mem(R, 9, I32), presence=mem(R, 2))
     bad(["inv_temperature", "divide"], inv_temperature=mem(4, 1))
@@ -142,7 +143,7 @@ def test_distill_refuses(emo, mem):
              lambda u, **kw: backward(emo, kw.pop("rows", N), kw.pop("vocab", V), u, stats=stats, grad=grad, **kw),
              lambda u, **kw: step(emo, kw.pop("rows", N), kw.pop("vocab", V), u, loss=loss, grad=grad, **kw))
     for call in calls:
-        for tau in (0.0, -1.0, float("inf"), float("nan")):
+        for tau in (0.0, -1.0, 1e-30, 1e30, float("inf"), float("nan")):
             refused(emo, call(t, tau=tau), "temperature")
         refused(emo, call(t, rows=-1), "rows")
         refused(emo, call(t, vocab=0), "vocab")
