@@ -467,6 +467,64 @@ def run_intervals(args, emo, synth, np, torch):
     print(json.dumps(out), flush=True)
 
 
+def run_propose(args, emo, synth, np, torch):
+    """A learned search (the other way for large graphs, Sec. VI-B) on workload k's graph: per step, draw
+    --propose candidates from the packs' logits (emo_adjust_logits with Gumbel noise), evaluate them, and
+    move the logits towards the 64 best (emo_distill_step on their level bytes).  Candidates over 1.05 T0
+    pay for it in proportion.  `value` = candidates drawn, evaluated and learned from per second, the
+    noise's generation included; `found` is the greedy policy after the last step."""
+    spec, B, K = synth.CONFIGS[args.workload], args.propose, min(64, args.propose)
+    g = synth.config_graph(args.workload)
+    P, F = g.num_packs, g.num_levels
+    gh = emo.EmoGraph(g, device=0)
+    dev = torch.device("cuda", 0)
+    top = torch.full((1, P), F - 1, dtype=torch.uint8, device=dev)
+    T0, E0 = (float(x.item()) for x in gh.eval_policies(top))
+    target = 1.05 * T0
+    logits, grad = torch.zeros((P, F), device=dev), torch.empty((P, F), device=dev)
+    loss = torch.empty(P, device=dev)
+    noise = torch.empty((B * P, F), device=dev)
+    levels = torch.empty((B, P), dtype=torch.uint8, device=dev)
+    T, E = torch.empty(B, device=dev), torch.empty(B, device=dev)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(spec.policy_seed)
+
+    def step():
+        noise.exponential_(generator=gen).log_().neg_()
+        emo.adjust_logits(logits, rows=B * P, noise=noise, choice=levels.view(-1))
+        gh.evaluate(levels, makespan=T, energy=E)
+        cost = E * (1.0 + 10.0 * ((T - target) / target).clamp_min(0.0))
+        best, at = torch.topk(cost, K, largest=False)
+        teacher = (best[0] - best) * (4.0 / (best[-1] - best[0]).clamp_min(1e-6))
+        emo.distill_step(logits, levels[at].t(), teacher, loss=loss, grad=grad)
+        logits.sub_(grad)
+
+    for _ in range(args.warmup):
+        step()
+    torch.cuda.synchronize()
+    t_wall = time.perf_counter()
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    for _ in range(args.steps):
+        step()
+    end.record()
+    torch.cuda.synchronize()
+    wall = time.perf_counter() - t_wall
+    ms_step = start.elapsed_time(end) / args.steps
+    emo.adjust_logits(logits, choice=levels[0])
+    Tf, Ef = (float(x.item()) for x in gh.eval_policies(levels[:1].contiguous()))
+    print(json.dumps({
+        "metric": "candidate policies drawn, evaluated and learned from/sec",
+        "value": B / (ms_step / 1e3), "unit": "policies/s", "n_gpus": 1, "steps": args.steps,
+        "warmup": args.warmup, "ms_per_step": ms_step, "higher_is_better": True, "scaling": "weak",
+        "vs_baseline": None, "dtype": "f32", "data": "synthetic",
+        "config": {"workload": spec.name, "candidates": B, "elites": K, "packs": P, "levels": F,
+                   "target_ratio": 1.05, "step": "emo_adjust_logits + emo_evaluate + emo_distill_step"},
+        "found": {"energy": Ef, "makespan": Tf, "energy_of_top_levels": E0, "makespan_of_top_levels": T0},
+        "wall_s": wall,
+    }), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -493,6 +551,9 @@ def main():
                     help="time the packing pass on --workload's graph (each pack one kernel)")
     ap.add_argument("--model", action="store_true",
                     help="time the pack model (NNLS, Eq. 7) for every pack of --workload")
+    ap.add_argument("--propose", type=int, default=0, metavar="B",
+                    help="time a learned search's step with B candidates on the workload's graph: levels "
+                         "drawn from logits, evaluated, the logits moved towards the best")
     ap.add_argument("--dp-buckets", type=int, default=64,
                     help="makespan buckets of the search between T0 and 1.05 T0 (default 64)")
     ap.add_argument("--calibrate-copy", type=int, default=0, metavar="MIB",
@@ -520,13 +581,16 @@ def main():
         print(json.dumps({"calibrate_copy_bytes": n, "launches": args.steps}))
         return
 
-    if (args.dp or args.intervals or args.pack or args.model) and args.workload == 0:
+    if (args.dp or args.intervals or args.pack or args.model or args.propose) and args.workload == 0:
         args.workload = 2
     if args.dp:
         run_dp(args, emo, synth, np, torch)
         return
     if args.intervals:
         run_intervals(args, emo, synth, np, torch)
+        return
+    if args.propose:
+        run_propose(args, emo, synth, np, torch)
         return
     if args.pack:
         run_pack(args, emo, synth, np, torch)
