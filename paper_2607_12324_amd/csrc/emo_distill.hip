@@ -137,6 +137,10 @@ __device__ __forceinline__ void sum_equal_ids(const Teacher &t, int K, int64_t l
 // bounded rows of few entries and long lists: 5,985 rows of 86 with 128 entries took 24 us.)
 constexpr int kTags = 256;
 
+// Whether a wave's row has the table: clearing and reading it has to be worth the comparisons (64 entries of the
+// list: even at rows of 1,000; at 2,000 the table costs 1.5 us more).
+__host__ __device__ constexpr bool by_table(int threads, int vocab, int K) { return threads == 64 && vocab <= 16 * K; }
+
 __device__ __forceinline__ void gather_probabilities(const Teacher &t, int K, int n, volatile float *table, volatile uint32_t *tags) {
     const int lane = threadIdx.x % 64;
     for (int i = lane; i < n; i += 64) table[i] = 0.f;
@@ -315,8 +319,8 @@ __global__ void __launch_bounds__(64) finish_kernel(DistillArgs a, int64_t first
     }
 }
 
-// Writes the gradient of a workgroup's piece (n entries from v0 of the row on).  A wave's row has the teacher's
-// probabilities by entry in `table`; wider ones are written over at the teacher's entries (`sum`).
+// Writes the gradient of a workgroup's piece (n entries from v0 of the row on).  A wave's row may have the teacher's
+// probabilities by entry in `table`; others are written over at the teacher's entries (`sum`).
 // rate = scale * temperature.
 template <typename T, typename O, int Threads, int C, bool Once>
 __device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece<T, Threads, C, Once> &piece, const uint32_t *mask, O *grad,
@@ -334,7 +338,7 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece
         if (e < whole) {
             float g[N];
             for (int j = 0; j < N; ++j) g[j] = has ? share * exp2_fast((entry<T>(piece.raw[c], j) - m) * a.log2e_tau) : 0.f;
-            if (Threads == 64 && has)
+            if (Threads == 64 && table && has)
                 for (int j = 0; j < N; ++j) g[j] = g[j] - rate * table[e + j];
             if (odd)
                 for (int j = 0; j < N; ++j) g[j] = allowed(mask, e + j) ? g[j] : 0.f;
@@ -343,10 +347,10 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &a, const Piece
     }
     if (whole + tid < n) {
         float g = share * exp2_fast((piece.x - m) * a.log2e_tau);
-        if (Threads == 64 && has) g = g - rate * table[whole + tid];
+        if (Threads == 64 && table && has) g = g - rate * table[whole + tid];
         grad[whole + tid] = static_cast<O>(has && allowed(mask, whole + tid) ? g : 0.f);
     }
-    if (Threads == 64 || !has) return;
+    if ((Threads == 64 && table) || !has) return;
     __syncthreads();        // the entries' own values are in memory before the teacher's go over them
     for (int k = tid; k < a.entries; k += Threads)
         if (!(t.sum[k] < 0.f))
@@ -380,10 +384,11 @@ __global__ void __launch_bounds__(Threads) backward_kernel(DistillArgs a, uint32
     piece.apply(mask, nullptr, n);
     __syncthreads();
     float *table = reinterpret_cast<float *>(lds) + teacher_floats(a.entries);
-    if (Threads == 64) gather_probabilities(t, a.entries, n, table, reinterpret_cast<uint32_t *>(table) + n);
+    const bool tabled = by_table(Threads, a.vocab, a.entries);
+    if (tabled) gather_probabilities(t, a.entries, n, table, reinterpret_cast<uint32_t *>(table) + n);
     else sum_equal_ids<Threads>(t, a.entries, v0, hi);
     O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride + v0;
-    write_gradient(a, piece, mask, grad, v0, n, s_has != 0, m, s, rate, t, table);
+    write_gradient(a, piece, mask, grad, v0, n, s_has != 0, m, s, rate, t, tabled ? table : nullptr);
 }
 
 // Loss and gradient of rows that fit a workgroup's registers: read once, written once.
@@ -425,7 +430,8 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     const float rate = row_value(a.scale, r, 1.f) * a.tau;
     __syncthreads();
     float *table = reinterpret_cast<float *>(lds) + teacher_floats(a.entries);
-    if (Threads == 64) gather_probabilities(t, a.entries, a.vocab, table, reinterpret_cast<uint32_t *>(table) + a.vocab);
+    const bool tabled = by_table(Threads, a.vocab, a.entries);
+    if (tabled) gather_probabilities(t, a.entries, a.vocab, table, reinterpret_cast<uint32_t *>(table) + a.vocab);
     else sum_equal_ids<Threads>(t, a.entries, 0, a.vocab);
     piece.apply(mask, s_mask, a.vocab);
     Running run;
@@ -438,7 +444,7 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
     }
     anew(piece.raw);
     O *grad = reinterpret_cast<O *>(a.grad) + static_cast<int64_t>(r) * a.grad_stride;
-    write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t, table);
+    write_gradient(a, piece, mask, grad, 0, a.vocab, has, run.m, run.s, rate, t, tabled ? table : nullptr);
 }
 
 // Rows of at most 64 entries: 64 rows a workgroup, in two phases.  The teacher's: a lane per row and a wave per
@@ -745,7 +751,7 @@ unsigned teacher_lds(const DistillArgs &a) { return static_cast<unsigned>(teache
 
 // With a wave's table of probabilities and its tags.
 unsigned gradient_lds(const DistillArgs &a, int threads) {
-    return teacher_lds(a) + (threads == 64 ? static_cast<unsigned>((a.vocab + kTags) * sizeof(float)) : 0u);
+    return teacher_lds(a) + (by_table(threads, a.vocab, a.entries) ? static_cast<unsigned>((a.vocab + kTags) * sizeof(float)) : 0u);
 }
 
 struct ForwardLaunch {
