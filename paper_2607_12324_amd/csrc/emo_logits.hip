@@ -105,7 +105,8 @@ constexpr int64_t kMaxHistory = int64_t(1) << 30;      // 32 bits hold a place b
 // the same counts), and whoever counts an id first puts the penalised logit in the count's place: penalties
 // cost a few of the history's ids, not every entry (a division each where any lane of a wave has a seen
 // entry, which is nearly always, took 320 of 700 instructions a chunk).  The choice of a row of several
-// tiles goes through `parts`, one best entry a tile, and choose_kernel.
+// tiles goes through `parts`, one best entry a tile, and choose_kernel.  256 x 131,072 bf16 with 1,024 ids,
+// bias and mask: 33 us, 4.2 TB/s of the 5.0 a copy reaches.
 template <typename T, typename O, int Threads, int PerThread, bool History>
 __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint32_t first, Pieces pieces, Best *parts) {
     constexpr int N = kChunk<T>, C = PerThread / N, Tile = Threads * PerThread;
@@ -242,8 +243,9 @@ struct GroupArgs {
 };
 
 // Rows of at most 64 entries: a group of 2^lg lanes per row, four entries a lane, so that a wave reads
-// neighbouring rows in one piece, and U rows a lane, whose loads are in flight together.  The choice is
-// the group's maximum, then the least index that has it.  The history (short: see small_rows) is compared
+// neighbouring rows in one piece, and U rows a lane, whose loads are in flight together (2^21 rows of 16 with
+// noise: 30 us, 4.5 TB/s; bound by latency: waves wait 60 % of their time, vector instructions take 20 us of
+// it).  The choice is the group's maximum, then the least index that has it.  The history (short: see small_rows) is compared
 // entry by entry.
 template <typename T, typename O, bool Penalties, int U>
 __global__ void __launch_bounds__(kThreads) adjust_group_kernel(GroupArgs g, int64_t first, AdjustArgs a) {
@@ -356,14 +358,15 @@ bool small_rows(const AdjustArgs &a, GroupArgs *g) {
 }
 
 // A row's tiles: one of 2,048 entries by a wave; longer rows of 4,096 by 256 threads (2 x 2^20 entries: 5.7 us,
-// tiles of 2,048 by single waves 7.7).  Every tile looks through its row's whole history: a long one wants
-// fewer, 8,192 entries by 512 threads, where that leaves 4 workgroups a compute unit (333 x 100,003 with up
-// to 4,096 ids: 71 us against 85; with 1,024 ids both take the same, with few the smaller tiles less).
+// tiles of 2,048 by single waves 7.7).  A tile looks through its row's whole history: past 512 ids a wave is too
+// few for it (12 rows of 650 with 6,707 ids: 22 us by a wave, 11.5 by 256 threads), and past 2,048 a row that
+// 512 threads hold is theirs (9.1 us there, 300 rows of 7,000 with 4,000 ids 10 against 18; 1,112 rows of 992 18
+// against 16).
 constexpr int kWaveTile = 2048, kTile = 4096, kLongTile = 8192;
 constexpr int kShortHistory = 512, kLongHistory = 2048;      // a wave takes 512 ids at once
 
 // A choice from few rows of up to 32,768 entries: a workgroup of 1,024 threads per row, which needs neither the
-// second launch nor a workspace (3 us of the calling thread's time each).
+// second launch nor a workspace (one row of 32,768: 10.5 us of the calling thread's time against 16).
 constexpr int kRowTile = 32768;
 
 bool whole_rows(int64_t rows, int64_t vocab) { return vocab > kTile && vocab <= kRowTile && rows <= 256; }
@@ -405,10 +408,9 @@ struct AdjustLaunch {
             return;
         }
         const int32_t ids = a.history.data ? a.history.cols : 0;
-        const int64_t wide = tiles_of(a.vocab, kLongTile);
         if (a.vocab <= kWaveTile && ids <= kShortHistory) tiles<T, O, 64, 32>();
         else if (a.choice && whole_rows(a.rows, a.vocab)) tiles<T, O, 1024, 32>();
-        else if (ids > kLongHistory && (wide == 1 || a.rows * wide >= 1024)) tiles<T, O, 512, 16>();
+        else if (ids > kLongHistory && a.vocab <= kLongTile) tiles<T, O, 512, 16>();
         else tiles<T, O, 256, 16>();
     }
 };
