@@ -504,8 +504,7 @@ def adjust_logits(logits, rows: int | None = None, *, history=None, lengths=None
         return _elsewhere(adjust_logits, logits, stream, rows, history=history, lengths=lengths, repetition=repetition,
                           frequency=frequency, presence=presence, bias=bias, inv_temperature=inv_temperature, mask=mask,
                           noise=noise, out=out, choice=choice, workspace=workspace)
-    if rows is None:
-        rows = n
+    rows = n if rows is None else int(rows)
     if out is None and choice is None:
         out = _torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
     ws, size, _keep = (None, 0, None) if choice is None else _workspace(workspace, lib.emo_adjust_workspace, rows, V, logits)
@@ -541,7 +540,7 @@ def distill_forward(logits, ids, teacher, temperature: float = 1.0, *, mask=None
     ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, logits)
     _check(lib.emo_distill_forward(
         N, V, _operand(logits, "logits", index), _operand(ids, "ids", index), _operand(teacher, "teacher", index),
-        temperature, None if mask is None else _operand(mask, "mask", index), _column(loss, "loss", index),
+        float(temperature), None if mask is None else _operand(mask, "mask", index), _column(loss, "loss", index),
         _operand(stats, "stats", index), ws, size, _raw_stream(index)))
     return loss, stats
 
@@ -557,7 +556,7 @@ def distill_backward(logits, stats, ids, teacher, temperature: float = 1.0, *, s
     grad = _torch.empty((N, V), dtype=logits.dtype, device=logits.device) if grad is None else grad
     _check(lib.emo_distill_backward(
         N, V, _operand(logits, "logits", index), _operand(stats, "stats", index), _operand(ids, "ids", index),
-        _operand(teacher, "teacher", index), temperature, None if scale is None else _column(scale, "scale", index),
+        _operand(teacher, "teacher", index), float(temperature), None if scale is None else _column(scale, "scale", index),
         None if mask is None else _operand(mask, "mask", index), _operand(grad, "grad", index), _raw_stream(index)))
     return grad
 
@@ -575,7 +574,7 @@ def distill_step(logits, ids, teacher, temperature: float = 1.0, *, scale=None, 
     ws, size, _keep = _workspace(workspace, lib.emo_distill_workspace, N, V, logits)
     _check(lib.emo_distill_step(
         N, V, _operand(logits, "logits", index), _operand(ids, "ids", index), _operand(teacher, "teacher", index),
-        temperature, None if scale is None else _column(scale, "scale", index),
+        float(temperature), None if scale is None else _column(scale, "scale", index),
         None if mask is None else _operand(mask, "mask", index), _column(loss, "loss", index),
         _operand(grad, "grad", index), ws, size, _raw_stream(index)))
     return loss, grad

@@ -189,6 +189,48 @@ def test_adjust_strided_operands(torch, emo):
         assert C.cpu().numpy().tolist() == (wc % 256).tolist()
 
 
+@pytest.mark.parametrize("V", [5, 16, 64, 71, 3001, 9001])
+def test_operands_of_fewer_rows(torch, emo, V):
+    """Every operand repeats over the call's rows by its own count, 1 and all among them; strided lists and outputs."""
+    rng = np.random.default_rng(V)
+    R = 12
+    counts = {"history": 4, "lengths": 6, "repetition": 3, "frequency": 1, "presence": 12, "bias": 2, "inv_temperature": 4,
+              "mask": 6, "noise": 3}
+    for turn in range(2):
+        x = rng.normal(size=(2 if turn else 4, V)).astype(np.float32)
+        kw = {k: rng.uniform(0.5, 1.5, size=n).astype(np.float32) for k, n in counts.items()
+              if k in ("repetition", "frequency", "presence", "inv_temperature")}
+        kw["history"] = rng.integers(-1, V + 1, size=(counts["history"], 10))
+        kw["lengths"] = rng.integers(0, 11, size=counts["lengths"]).astype(np.int32)
+        kw["bias"] = rng.normal(size=(counts["bias"], V)).astype(np.float32)
+        kw["noise"] = rng.gumbel(size=(counts["noise"], V)).astype(np.float32)
+        kw["mask"] = orc.mask_words(rng.random((counts["mask"], V)) < 0.7)
+        want, wc = orc.adjust(R, x, **kw)
+        d = {k: dev(torch, v) for k, v in kw.items()}
+        d["history"] = torch.stack([d["history"], d["history"] + 7], 2)[:, :, 0]        # every other element
+        O, C = emo.adjust_logits(dev(torch, x), rows=R, out=torch.empty((R, V), device="cuda"),
+                                 choice=torch.empty((R, 3), dtype=torch.int32, device="cuda")[:, 1], **d)
+        bits_equal(torch, O, want, "f32", "adjusted")
+        assert C.cpu().tolist() == wc.tolist()
+        counts = {k: 12 // n for k, n in counts.items()}
+    N, K = 12, 7
+    x = rng.normal(size=(N, V)).astype(np.float32)
+    i, t = rng.integers(0, V, size=(3, K)), rng.normal(size=(4, K)).astype(np.float32)
+    words, scale = orc.mask_words(rng.random((6, V)) < 0.8), rng.uniform(size=2).astype(np.float32)
+    w = orc.distill(x, i, t, 1.3, words, scale)
+    _, tl, tg = bounds(w, V, K, 1.3, 1.3 * np.tile(scale, 6).astype(np.float64), "f32")
+    I = torch.stack([dev(torch, i, "i64")] * 2, 2)[:, :, 0]
+    T = torch.stack([dev(torch, t)] * 3, 2)[:, :, 2]
+    loss, stats = torch.empty((N, 2), device="cuda")[:, 1], torch.empty((N, 5), device="cuda")[:, 2:4]
+    X, M, S = dev(torch, x), dev(torch, words), dev(torch, scale)
+    emo.distill_forward(X, I, T, 1.3, mask=M, loss=loss, stats=stats)
+    g = emo.distill_backward(X, stats, I, T, 1.3, scale=S, mask=M)
+    loss2, g2 = emo.distill_step(X, I, T, np.float32(1.3), scale=S, mask=M)
+    for a, b in ((loss, g), (loss2, g2)):
+        check_near(a.cpu().numpy(), w["loss"], tl, "loss")
+        check_near(b.cpu().numpy(), w["grad"], tg, "gradient")
+
+
 def test_adjust_defaults_and_refusals(torch, emo):
     x = torch.randn(4, 300, device="cuda", dtype=torch.float16)
     out, choice = emo.adjust_logits(x)
