@@ -42,6 +42,7 @@ __device__ __forceinline__ float block_reduce(float x, float *s_red) {
     return x;
 }
 
+// The hardware's 2^x: within a unit in the last place, 0 below 2^-126.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A row's teacher in LDS, K places each: the entry's id (-1: does not count), its probability, the logit at
@@ -649,7 +650,7 @@ __global__ void __launch_bounds__(kThreads) small_kernel(SmallArgs a, int64_t fi
             to[1] = s[u];
         }
         if (Forward && a.loss) {
-            const float log_s = 0.69314718f * __builtin_amdgcn_logf(s[u]);
+            const float log_s = 0.69314718f * __builtin_amdgcn_logf(s[u]);      // the hardware's log2, within a unit or so
             float loss = 0.f;
             for (int j = 0; j < 4; ++j)
                 if (p[j] != 0.f) loss += p[j] * (log_s - (x[u][j] - m[u]) * a.inv_tau);

@@ -315,6 +315,29 @@ def test_distill_teachers_of_nan_and_infinity(torch, emo):
             assert np.isnan(b[:3, 1]).all() and np.isfinite(b[3:]).all()
 
 
+def test_workspaces_of_the_caller(torch, emo):
+    """A workspace given serves call after call whatever it holds; too small a one is refused."""
+    import ctypes
+    for call, size in ((lambda x, w: emo.adjust_logits(x, choice=torch.empty(len(x), dtype=torch.int64, device="cuda"), workspace=w)[1],
+                        emo.lib.emo_adjust_workspace),
+                       (lambda x, w: emo.distill_forward(x, torch.full((1, 1), 5, device="cuda"), torch.zeros((1, 1), device="cuda"),
+                                                         workspace=w)[0], emo.lib.emo_distill_workspace),
+                       (lambda x, w: emo.distill_step(x, torch.full((1, 1), 5, device="cuda"), torch.zeros((1, 1), device="cuda"),
+                                                      workspace=w)[1], emo.lib.emo_distill_workspace)):
+        n = ctypes.c_int64(0)
+        for V in (200000, 70001):
+            x = torch.randn((3, V), device="cuda")
+            assert size(3, V, ctypes.byref(n)) == 0 and n.value > 0
+            w = torch.full((n.value,), 255, dtype=torch.uint8, device="cuda")
+            want = call(x, None)
+            for _ in range(2):
+                assert torch.equal(call(x, w), want)
+            with pytest.raises(emo.EmoError, match="workspace"):
+                call(x, w[: n.value - 1])
+            with pytest.raises(ValueError, match="workspace"):
+                call(x, torch.zeros(2 * n.value, dtype=torch.uint8, device="cuda")[::2])
+
+
 def test_adjust_masks_that_leave_little(torch, emo):
     """Nothing, only -inf, only the lowest value, only NaN; a byte choice without an entry is 255."""
     for V in (5, 70, 5000):
