@@ -819,6 +819,7 @@ struct StepLaunch {
         if (a.vocab <= 2048) rows<T, O, 64, 32>();
         else if (a.vocab <= 4096) rows<T, O, 128, 32>();
         else if (a.vocab <= 8192) rows<T, O, 256, 32>();
+        else if (a.vocab <= 16384) rows<T, O, 512, 32>();
         else if (a.vocab <= 32768) rows<T, O, 512, 64>();
         else if constexpr (sizeof(T) == 4) rows<T, O, 1024, 64>();
         else if (a.vocab <= 65536) rows<T, O, 512, 128>();

@@ -369,7 +369,9 @@ constexpr int kShortHistory = 512, kLongHistory = 2048;      // a wave takes 512
 // second launch nor a workspace (one row of 32,768: 10.5 us of the calling thread's time against 16).
 constexpr int kRowTile = 32768;
 
-bool whole_rows(int64_t rows, int64_t vocab) { return vocab > kTile && vocab <= kRowTile && rows <= 256; }
+constexpr int kMiddleTile = 16384;
+
+bool whole_rows(int64_t rows, int64_t vocab) { return vocab > kTile && (vocab <= kMiddleTile || (vocab <= kRowTile && rows <= 256)); }
 
 int64_t tiles_of(int64_t vocab, int tile) { return (vocab + tile - 1) / tile; }
 
@@ -409,8 +411,9 @@ struct AdjustLaunch {
         }
         const int32_t ids = a.history.data ? a.history.cols : 0;
         if (a.vocab <= kWaveTile && ids <= kShortHistory) tiles<T, O, 64, 32>();
-        else if (a.choice && whole_rows(a.rows, a.vocab)) tiles<T, O, 1024, 32>();
         else if (ids > kLongHistory && a.vocab <= kLongTile) tiles<T, O, 512, 16>();
+        else if (a.choice && whole_rows(a.rows, a.vocab) && a.vocab <= kMiddleTile) tiles<T, O, 512, 32>();
+        else if (a.choice && whole_rows(a.rows, a.vocab)) tiles<T, O, 1024, 32>();
         else tiles<T, O, 256, 16>();
     }
 };
