@@ -477,6 +477,32 @@ def test_distill_rows(torch, emo, N, V, K, dtype):
     check_distill(torch, emo, rng, N, V, K, dtype, "i32", mask=N if V < 1000 else 1, tau=2.0)
 
 
+@pytest.mark.parametrize("N,V", [(4200, 2500), (2100, 4200), (1100, 8300), (8300, 2051), (4200, 4097), (2100, 8193)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_distill_many_rows(torch, emo, N, V, dtype):
+    """More rows than the card holds at once: against the two passes on every row, the oracle on some."""
+    rng = np.random.default_rng(N)
+    x = torch.from_numpy(rng.normal(size=(N, V)).astype(np.float32) * 3).to(types(torch)[dtype])
+    i, t = rng.integers(-1, V, size=(N, 9)), rng.normal(size=(N, 9)).astype(np.float32)
+    i[:, 3] = i[:, 5]
+    words = orc.mask_words(rng.random((1, V)) < 0.8)
+    X, I, T, M = x.cuda(), dev(torch, i, "i32"), dev(torch, t), dev(torch, words)
+    loss, stats = emo.distill_forward(X, I, T, mask=M)
+    g = emo.distill_backward(X, stats, I, T, mask=M)
+    loss2, g2 = emo.distill_step(X, I, T, mask=M)
+    some = rng.choice(N, 6, replace=False)
+    w = orc.distill(x.float().numpy()[some], i[some], t[some], 1.0, words)
+    _, tl, tg = bounds(w, V, 9, 1.0, np.ones(6), dtype)
+    for a, b in ((loss, g), (loss2, g2)):
+        check_near(a.cpu().numpy()[some], w["loss"], tl, "loss")
+        check_near(b.float().cpu().numpy()[some], w["grad"], tg, "gradient")
+    # the two differ by their roundings: each is within the bounds of the exact values, s by V / 256 + 67 steps
+    near = 2 * (V / 256 + 67 + 60) * EPS
+    assert bool(((loss - loss2).abs() <= near * (1 + loss.abs())).all())
+    q = g.float().abs() + 1e-3
+    assert bool(((g.float() - g2.float()).abs() <= q * (near + 2 * HALF[dtype])).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("V", [9, 64, 1031, 50021, 140001])
 def test_distill_in_place_and_strides(torch, emo, dtype, V):
