@@ -806,9 +806,9 @@ struct StepLaunch {
     hipStream_t st;
 
     // Whether there are more rows than the card holds workgroups of that many threads (2,048 threads a compute
-    // unit; twice that for 4-byte types, whose entries take the registers of a wave in two).  Then half the
-    // threads with 64 entries each: a row takes about as long, its latencies above all, and twice the rows
-    // are on their way (3,000 x 9,333 bf16: 38 us against 47; 300 rows: 12.2 against 11.8; 3,000 x 9,333 fp32:
+    // unit; from twice as many for 4-byte types, whose 64 entries a lane take twice the registers, so that
+    // fewer waves stay).  Then half the threads with 64 entries each: a row takes about as long, its latencies
+    // above all, and more rows are on their way (3,000 x 9,333 bf16: 38 us against 47; 300 rows: 12.2 against 11.8; 3,000 x 9,333 fp32:
     // 54 against 61, 1,500 rows 33 against 31).
     template <typename T>
     bool more_than_held(int threads) const {
