@@ -837,7 +837,9 @@ struct StepLaunch {
     }
 };
 
-// The operands every distillation call has.
+// The operands every distillation call has; the logits' range is the first.
+constexpr int kLogitsRange = 0;
+
 emo_status distill_operands(Checker &c, DistillArgs &a, int64_t rows, int64_t vocab, const emo_tensor *logits,
                             const emo_tensor *ids, const emo_tensor *teacher, float temperature, const emo_tensor *mask) {
     emo_status s = check_sizes(rows, vocab);
@@ -883,7 +885,7 @@ emo_status emo_distill_forward(int64_t rows, int64_t vocab, const emo_tensor *lo
     const Mat l = c.take("loss", loss, bit(EMO_F32), 1, false, true);
     const Mat st = c.take("stats", stats, bit(EMO_F32), 2, true, true);
     if (rows > 0) c.workspace(workspace, workspace_bytes, distill_bytes(rows, vocab));
-    s = c.apart(nullptr, nullptr);
+    s = c.apart(-1, -1);
     if (s != EMO_OK) return s;
     if (rows == 0 || (!loss && !stats)) return emo::report(EMO_OK, "");
     a.loss = const_cast<char *>(l.data);
@@ -907,7 +909,8 @@ emo_status emo_distill_backward(int64_t rows, int64_t vocab, const emo_tensor *l
         return fail(EMO_ERR_INVALID_ARGUMENT, "stats has %lld rows, needs %lld", (long long)stats->rows, (long long)rows);
     a.scale = c.take("scale", scale, bit(EMO_F32), 1, false, false);
     const Mat g = c.take("gradient", gradient, kFloats, vocab, true, true);
-    s = c.apart(gradient, logits);
+    const int twin = c.last;
+    s = c.apart(twin, kLogitsRange);
     if (s == EMO_OK) s = check_written(gradient, logits, "gradient");
     if (s != EMO_OK) return s;
     if (rows == 0) return emo::report(EMO_OK, "");
@@ -929,8 +932,9 @@ emo_status emo_distill_step(int64_t rows, int64_t vocab, const emo_tensor *logit
     a.scale = c.take("scale", scale, bit(EMO_F32), 1, false, false);
     const Mat l = c.take("loss", loss, bit(EMO_F32), 1, false, true);
     const Mat g = c.take("gradient", gradient, kFloats, vocab, true, true);
+    const int twin = c.last;
     if (rows > 0) c.workspace(workspace, workspace_bytes, distill_bytes(rows, vocab));
-    s = c.apart(gradient, logits);
+    s = c.apart(twin, kLogitsRange);
     if (s == EMO_OK) s = check_written(gradient, logits, "gradient");
     if (s != EMO_OK) return s;
     if (rows == 0) return emo::report(EMO_OK, "");

@@ -403,6 +403,7 @@ struct Checker {
         const emo_tensor *t;
     } ranges[16];
     int n = 0;
+    int last = -1;      // the range of the operand taken last, -1 if it has none
 
     void bad(emo_status s) {
         if (status == EMO_OK) status = s;
@@ -411,6 +412,7 @@ struct Checker {
     // An operand (absent when t is NULL) of `cols` columns (-1: any).  Outputs have all rows.
     Mat take(const char *name, const emo_tensor *t, unsigned types, int64_t cols, bool dense, bool output) {
         Mat m = {};
+        last = -1;
         if (!t || status != EMO_OK) return m;
         if (t->dtype < EMO_F32 || t->dtype > EMO_I64 || !(types & bit(t->dtype)))
             return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s has a type that this call does not take (%d)", name, (int)t->dtype)), m;
@@ -443,11 +445,14 @@ struct Checker {
         const int64_t size = size_of(t->dtype);
         const uintptr_t p = reinterpret_cast<uintptr_t>(t->data);
         if (p % size) return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s is not aligned to its elements", name)), m;
-        const __int128 last = static_cast<__int128>(t->rows - 1) * t->row_stride + static_cast<__int128>(t->cols - 1) * t->col_stride;
-        if (last >= (static_cast<__int128>(1) << 48))
+        const __int128 end = static_cast<__int128>(t->rows - 1) * t->row_stride + static_cast<__int128>(t->cols - 1) * t->col_stride;
+        if (end >= (static_cast<__int128>(1) << 48))
             return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s spans more than an address space", name)), m;
         m.data = static_cast<const char *>(t->data);
-        if (n < 16) ranges[n++] = {name, p, p + static_cast<uintptr_t>((static_cast<int64_t>(last) + 1) * size), output, t};
+        if (n < 16) {
+            last = n;
+            ranges[n++] = {name, p, p + static_cast<uintptr_t>((static_cast<int64_t>(end) + 1) * size), output, t};
+        }
         return m;
     }
 
@@ -460,15 +465,16 @@ struct Checker {
         if (n < 16) ranges[n++] = {"workspace", b, b + static_cast<uintptr_t>(need), true, nullptr};
     }
 
-    // Outputs lie apart from everything else; `twin` may be the very memory of `of`.
-    emo_status apart(const emo_tensor *twin, const emo_tensor *of) {
+    // Outputs lie apart from everything else; the output of range `twin` may be the very memory of range `of`
+    // (-1: none may).  The ranges name the operands: records do not, since one can describe several.
+    emo_status apart(int twin, int of) {
         if (status != EMO_OK) return status;
         for (int i = 0; i < n; ++i)
             for (int j = 0; j < n; ++j) {
                 if (i == j || !ranges[i].output || ranges[i].begin >= ranges[j].end || ranges[j].begin >= ranges[i].end) continue;
                 const emo_tensor *x = ranges[i].t, *y = ranges[j].t;
-                if (twin && x && y && ((x == twin && y == of) || (x == of && y == twin)) && x->data == y->data && x->dtype == y->dtype &&
-                    x->rows == y->rows && x->cols == y->cols && (x->rows == 1 || x->row_stride == y->row_stride))
+                if (i == twin && j == of && x->data == y->data && x->dtype == y->dtype && x->rows == y->rows && x->cols == y->cols &&
+                    (x->rows == 1 || x->row_stride == y->row_stride))
                     continue;
                 return status = fail(EMO_ERR_INVALID_ARGUMENT, "%s overlaps %s", ranges[i].name, ranges[j].name);
             }

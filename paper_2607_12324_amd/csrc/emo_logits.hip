@@ -451,6 +451,7 @@ emo_status emo_adjust_logits(int64_t rows, int64_t vocab, const emo_tensor *logi
     a.rows = static_cast<uint32_t>(rows);
     a.vocab = static_cast<int32_t>(vocab);
     a.logits = c.take("logits", logits, kFloats, vocab, true, false);
+    const int of = c.last;
     a.history = c.take("history", history, kIndices, -1, false, false);
     a.lengths = c.take("lengths", lengths, bit(EMO_I32), 1, false, false);
     a.repetition = c.take("repetition", repetition, bit(EMO_F32), 1, false, false);
@@ -461,9 +462,10 @@ emo_status emo_adjust_logits(int64_t rows, int64_t vocab, const emo_tensor *logi
     a.mask = c.take("mask", mask, bit(EMO_I32), (vocab + 31) / 32, true, false);
     a.noise = c.take("noise", noise, bit(EMO_F32), vocab, true, false);
     const Mat o = c.take("out", out, kFloats, vocab, true, true);
+    const int twin = c.last;
     const Mat ch = c.take("choice", choice, kIndices, 1, false, true);
     if (rows > 0 && choice) c.workspace(workspace, workspace_bytes, adjust_bytes(rows, vocab));
-    s = c.apart(out, logits);
+    s = c.apart(twin, of);
     if (s == EMO_OK) s = check_written(out, logits, "out");
     if (s != EMO_OK) return s;
     if (rows == 0 || (!out && !choice)) return emo::report(EMO_OK, "");

@@ -118,6 +118,19 @@ def test_adjust_refuses_overlaps(emo, mem):
         refused(emo, adjust(emo, R, V, **kw), "overlaps")
 
 
+def test_adjust_in_place_frees_no_other_operand(emo, mem):
+    """The adjusted logits may be the logits, not the noise or the bias, whichever records describe them."""
+    R, V = 6, 100
+    x = mem(R, V)
+    again = emo.Tensor(x.data, R, V, V, 1, F32, 0)
+    choice = mem(R, 1, I32)
+    for out in (x, again):
+        for other in (x, again):
+            refused(emo, adjust(emo, R, V, logits=x, noise=other, out=out, choice=choice), "out overlaps noise")
+            refused(emo, adjust(emo, R, V, logits=x, bias=other, out=out, choice=choice), "out overlaps bias")
+            refused(emo, adjust(emo, R, V, logits=mem(R, V), noise=other, out=out, choice=choice), "out overlaps noise")
+
+
 DIST = ("logits", "ids", "teacher")
 
 
@@ -167,6 +180,18 @@ def test_distill_refuses(emo, mem):
     refused(emo, step(emo, N, V, t, loss=loss, grad=None), "NULL")
     refused(emo, step(emo, N, V, t, grad=mem(N, V, data=t["logits"].data + 4)), "overlaps")
     refused(emo, step(emo, N, V, t, grad=mem(N, V, data=t["teacher"].data)), "overlaps")
+
+
+def test_distill_in_place_frees_no_other_operand(emo, mem):
+    """The gradient may be the logits, not the teacher, whichever records describe them."""
+    N, V = 6, 5
+    x = mem(N, V)
+    again = emo.Tensor(x.data, N, V, V, 1, F32, 0)
+    for grad in (x, again):
+        for teacher in (x, again):
+            t = {"logits": x, "ids": mem(N, V, I32), "teacher": teacher}
+            refused(emo, step(emo, N, V, t, loss=mem(N, 1), grad=grad), "gradient overlaps teacher")
+            refused(emo, backward(emo, N, V, t, stats=mem(N, 2), grad=grad), "gradient overlaps teacher")
 
 
 def test_workspaces(emo, mem):
