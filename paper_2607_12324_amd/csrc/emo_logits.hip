@@ -95,7 +95,12 @@ __device__ __forceinline__ int32_t live_history(const AdjustArgs &a, uint32_t r)
     return a.lengths.data ? min(max(*row_of<int32_t>(a.lengths, r), 0), L) : L;
 }
 
+// What a tile's table holds of an entry: kUnseen plus its count, then the bits of the penalised logit.  kUnseen's
+// bits are a NaN too, which a rate may hand on, so a NaN is kept as the usual one.
 constexpr uint32_t kUnseen = 0xffffffffu;
+
+__device__ __forceinline__ uint32_t seen_bits(float x) { return x != x ? 0x7fc00000u : __float_as_uint(x); }
+
 constexpr int64_t kMaxHistory = int64_t(1) << 30;      // 32 bits hold a place beyond the last id that a thread asks for
 
 // A workgroup per tile of Threads * PerThread entries of a row.  Bound by memory and, with a history, by what
@@ -170,16 +175,16 @@ __global__ void __launch_bounds__(Threads) adjust_tile_kernel(AdjustArgs a, uint
             if (L <= (Held + 64) * Threads) {
 #pragma unroll
                 for (int h = 0; h < Held; ++h)
-                    if (id[h] >= 0) s_seen[id[h]] = __float_as_uint(penalise(a, rate, held[h], s_seen[id[h]] + 1));
+                    if (id[h] >= 0) s_seen[id[h]] = seen_bits(penalise(a, rate, held[h], s_seen[id[h]] + 1));
                 for (; mine; mine &= mine - 1) {
                     const int32_t i = tid + (Held + __builtin_ctzll(mine)) * Threads;
                     const int32_t e = load_id(a.history, hrow, i, a.vocab) - v0;
-                    s_seen[e] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
+                    s_seen[e] = seen_bits(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
                 }
             } else {
                 for (int e = tid; e < n; e += Threads)
                     if (s_seen[e] != kUnseen)
-                        s_seen[e] = __float_as_uint(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
+                        s_seen[e] = seen_bits(penalise(a, rate, static_cast<float>(logits[e]), s_seen[e] + 1));
             }
             __syncthreads();
         }

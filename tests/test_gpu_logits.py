@@ -266,6 +266,27 @@ def test_adjust_odd_rates(torch, emo, V):
         assert C.cpu().tolist() == wc.tolist()
 
 
+@pytest.mark.parametrize("L", [20, 1500, 40000])
+@pytest.mark.parametrize("V", [40, 70, 3001, 9001, 40001])
+def test_adjust_rates_that_are_no_number(torch, emo, V, L):
+    """A penalty of any NaN, that of all ones among them, makes the entry NaN: the ids, of the greatest logits, are
+    the history's last, each once."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(size=(4, V)).astype(np.float32)
+    h = np.full((4, L), -1)
+    for r in range(4):
+        h[r, -20:] = rng.choice(V, 20, replace=False)
+        x[r, h[r, -20:]] += 20
+    nans = np.array([0xffffffff, 0x7fffffff, 0x7fc00000, 0xffc00001], np.uint32).view(np.float32)
+    for name in ("repetition", "frequency", "presence"):
+        want, wc = orc.adjust(4, x, history=h, **{name: nans})
+        assert np.isnan(want).sum() == 80
+        O, C = emo.adjust_logits(dev(torch, x), history=dev(torch, h, "i32"), out=torch.empty((4, V), device="cuda"),
+                                 choice=torch.empty(4, dtype=torch.int32, device="cuda"), **{name: dev(torch, nans)})
+        bits_equal(torch, O, want, "f32", f"adjusted, {name}")
+        assert C.cpu().tolist() == wc.tolist()
+
+
 @pytest.mark.parametrize("V", [2, 7, 40, 61, 75, 2500, 9003, 33001])
 def test_adjust_odd_noise_bias_and_mask_ends(torch, emo, V):
     """Infinities and NaN in noise and bias; mask bits behind the last entry, which are nobody's."""
