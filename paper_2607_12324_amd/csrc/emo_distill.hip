@@ -9,7 +9,7 @@ struct DistillArgs {
     uint32_t rows;
     int32_t vocab;
     int32_t entries;        // K
-    float inv_tau, tau;     // 1 / temperature, temperature
+    float tau;              // temperature
     float log2e_tau;        // log2(e) / temperature: exp(d / temperature) = 2^(d * log2e_tau)
     Mat logits, ids, teacher, mask, scale, stats;
     char *loss, *stats_out, *grad;
@@ -164,13 +164,14 @@ __device__ __forceinline__ void gather_probabilities(const Teacher &t, int K, in
     }
 }
 
-// The loss, by one wave: the entries' distances below the row's logarithm of sums.
+// The loss, by one wave: the entries' distances below the row's logarithm of sums, in units of the logits, so that
+// one of the lowest value's size is no infinity below a temperature of 1.
 __device__ __forceinline__ float teacher_loss(const DistillArgs &a, const Teacher &t, float m, float s) {
-    const float log_s = logf(s);
+    const float log_s = logf(s) * a.tau;
     float loss = 0.f;
     for (int k = threadIdx.x % 64; k < a.entries; k += 64)
-        if (t.id[k] >= 0 && t.p[k] != 0.f) loss += t.p[k] * (log_s - (t.x[k] - m) * a.inv_tau);
-    return wave_sum(loss) * a.tau * a.tau;
+        if (t.id[k] >= 0 && t.p[k] != 0.f) loss += t.p[k] * (log_s - (t.x[k] - m));
+    return wave_sum(loss) * a.tau;
 }
 
 __device__ __forceinline__ void store_stats(const DistillArgs &a, uint32_t r, float m, float s) {
@@ -458,7 +459,7 @@ __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t fi
 struct SmallArgs {
     int32_t lg, vocab, entries;
     uint32_t rows;
-    float inv_tau, tau, log2e_tau;
+    float tau, log2e_tau;
     Rows logits, ids, teacher, mask, scale, stats;
     uint32_t id_step, teacher_step;     // bytes from one entry to the next
     int32_t id_type, teacher_type;
@@ -650,11 +651,11 @@ __global__ void __launch_bounds__(kThreads) small_kernel(SmallArgs a, int64_t fi
             to[1] = s[u];
         }
         if (Forward && a.loss) {
-            const float log_s = 0.69314718f * __builtin_amdgcn_logf(s[u]);      // the hardware's log2, within a unit or so
+            const float log_s = 0.69314718f * __builtin_amdgcn_logf(s[u]) * a.tau;     // the hardware's log2, within a unit or so
             float loss = 0.f;
             for (int j = 0; j < 4; ++j)
-                if (p[j] != 0.f) loss += p[j] * (log_s - (x[u][j] - m[u]) * a.inv_tau);
-            loss = group_sum(loss, a.lg) * a.tau * a.tau;
+                if (p[j] != 0.f) loss += p[j] * (log_s - (x[u][j] - m[u]));      // in the logits' units: see teacher_loss
+            loss = group_sum(loss, a.lg) * a.tau;
             if (v == 0) *reinterpret_cast<float *>(a.loss + static_cast<uint64_t>(r) * a.loss_stride) = has ? loss : 0.f;
         }
         if (Backward && mine) {
@@ -719,7 +720,6 @@ bool small_rows(const DistillArgs &a, int32_t grad_size, SmallArgs *s) {
     s->vocab = a.vocab;
     s->entries = a.entries;
     s->rows = a.rows;
-    s->inv_tau = a.inv_tau;
     s->tau = a.tau;
     s->log2e_tau = a.log2e_tau;
     s->id_step = static_cast<uint32_t>(id_step);
@@ -845,7 +845,7 @@ emo_status distill_operands(Checker &c, DistillArgs &a, int64_t rows, int64_t vo
     emo_status s = check_sizes(rows, vocab);
     if (s != EMO_OK) return s;
     if (!logits || !ids || !teacher) return fail(EMO_ERR_INVALID_ARGUMENT, "logits, ids or teacher is NULL");
-    // its square and inverse are fp32 numbers with room
+    // its square and log2(e) divided by it are fp32 numbers with room
     if (!(temperature >= 0x1p-60f && temperature <= 0x1p60f))
         return fail(EMO_ERR_INVALID_ARGUMENT, "temperature must be in [2^-60, 2^60]");
     if (ids->cols < 0 || ids->cols > kMaxEntries)
@@ -855,7 +855,6 @@ emo_status distill_operands(Checker &c, DistillArgs &a, int64_t rows, int64_t vo
     a.vocab = static_cast<int32_t>(vocab);
     a.entries = static_cast<int32_t>(ids->cols);
     a.tau = temperature;
-    a.inv_tau = static_cast<float>(1.0 / static_cast<double>(temperature));
     a.log2e_tau = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
     a.logits = c.take("logits", logits, kFloats, vocab, true, false);
     if (c.status == EMO_OK && rows > 0 && logits->rows != rows)

@@ -597,6 +597,30 @@ def test_distill_specials(torch, emo, V):
         assert not b[[0, 4]].any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [12, 60, 500, 6000, 90000])
+def test_distill_teachers_on_the_lowest_value(torch, emo, V, dtype):
+    """The teacher on logits of the type's lowest value, as masks by addition leave them: the distance in
+    temperatures is no fp32 number below a temperature of 1, but the loss, temperature times the distance, is."""
+    rng = np.random.default_rng(V)
+    N, K, tau = 40, 5, 0.25
+    x = as_f32(torch, rng.normal(size=(N, V)).astype(np.float32), dtype)
+    i = np.stack([rng.choice(V, K, replace=False) for _ in range(N)])
+    t = rng.normal(size=(N, K)).astype(np.float32) * 0.25
+    for r in range(N):
+        x[r, i[r, :1 + r % 4]] = float(torch.finfo(types(torch)[dtype]).min)
+    w = orc.distill(x, i, t, tau)
+    assert np.isfinite(w["loss"]).all() and w["loss"].min() > 1e33
+    _, tl, tg = bounds(w, V, K, tau, np.full(N, tau), dtype)
+    X, I, T = dev(torch, x, dtype), dev(torch, i, "i32"), dev(torch, t)
+    loss, stats = emo.distill_forward(X, I, T, tau)
+    g = emo.distill_backward(X, stats, I, T, tau)
+    loss2, g2 = emo.distill_step(X, I, T, tau)
+    for a, b in ((loss, g), (loss2, g2)):
+        check_near(a.cpu().numpy(), w["loss"], tl, "loss")
+        check_near(b.float().cpu().numpy(), w["grad"], tg, "gradient")
+
+
 def test_streams_and_graphs(torch, emo):
     """Calls on side streams at once, each with its own operands, and captured graphs replayed between eager
     calls give the same bits as the eager calls."""
