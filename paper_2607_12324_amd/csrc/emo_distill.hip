@@ -201,7 +201,10 @@ __device__ __forceinline__ void anew(u32x4 (&raw)[C]) {
     for (int c = 0; c < C; ++c) asm volatile("" : "+v"(raw[c]));
 }
 
-// Adds the entries of C chunks and one more: one maximum and one change of origin for all of them.
+// Adds the entries of C chunks and one more: one maximum and one change of origin for all of them.  A chunk's
+// exponentials are summed by themselves, then the chunks, then these sums: a row's additions follow each other by
+// these few steps, where one running sum rounded each entry at the size of all before (131,072 equal entries by
+// 256 threads: 6e-6 of s, now 2e-7).
 template <typename T, int C>
 __device__ __forceinline__ void add_entries(Running &run, u32x4 (&raw)[C], float x, float log2e_tau) {
     constexpr int N = kChunk<T>;
@@ -213,13 +216,17 @@ __device__ __forceinline__ void add_entries(Running &run, u32x4 (&raw)[C], float
     }
     anew(raw);
     const float o = origin(m);
-    float s = run.s * exp2_fast((run.m - o) * log2e_tau) + exp2_fast((x - o) * log2e_tau);
+    const float before = run.s * exp2_fast((run.m - o) * log2e_tau);
+    float s = exp2_fast((x - o) * log2e_tau);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        for (int j = 0; j < N; ++j) s += exp2_fast((entry<T>(raw[c], j) - o) * log2e_tau);
+        float sum = exp2_fast((entry<T>(raw[c], 0) - o) * log2e_tau);
+        for (int j = 1; j < N; ++j) sum += exp2_fast((entry<T>(raw[c], j) - o) * log2e_tau);
+        s += sum;
         __builtin_amdgcn_sched_barrier(0);
     }
     anew(raw);
+    s += before;
     asm volatile("" : "+v"(s));     // summed here, not where it is read: the exponents of all entries would live until then
     run = {m, s};
 }

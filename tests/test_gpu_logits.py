@@ -482,6 +482,26 @@ def test_distill_sizes(torch, emo, V):
     check_distill(torch, emo, rng, 3, V, 17, "f16", "u8", mask=1, tau=0.5, grad="f32", shared=True, stride=V + 5, offset=3)
 
 
+@pytest.mark.parametrize("V", [32768, 131072])
+def test_distill_long_sums(torch, emo, V):
+    """Rows of one value below the greatest, whose exponential a long running sum would round the same way every
+    time: of 131,072 entries such a sum is off by 105 half steps.  Its additions here follow each other by 4 within 16
+    bytes, 8 times 16 bytes, V / 8,192 steps, 6 in a wave, 4 waves; an exponential is off by its argument's 3
+    roundings (the argument is below 0.02) and a step, two half steps."""
+    steps = 2.0 ** 15                   # of a sum from 256 on: one below the next half, so that it is rounded down
+    e = (np.floor(0.99 * steps) + 0.45) / steps
+    x = np.full((1, V), np.log(e), np.float32)
+    x[0, :1024] = 0.0                   # 16 bytes of every thread
+    X = dev(torch, x).expand(2048, V)
+    I, T = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.zeros((1, 1), device="cuda")
+    loss, stats = emo.distill_forward(X, I, T)
+    w = orc.distill(x, np.zeros((1, 1), int), np.zeros((1, 1)), 1.0)
+    near = (4 + 8 + V / 8192 + 6 + 4 + 3 * 0.02 + 2) * EPS
+    check_near(stats[:, 1].cpu().numpy(), np.full(2048, w["stats"][0, 1]), near * w["stats"][0, 1], "s")
+    # log s is off by s's error and a rounding of its own, the distance and the product by one each
+    check_near(loss.cpu().numpy(), np.full(2048, w["loss"][0]), near + 4 * EPS * w["loss"][0], "loss")
+
+
 @pytest.mark.parametrize("K", [0, 1, 2, 63, 64, 65, 100, 255, 256, 257, 1000, 1024])
 @pytest.mark.parametrize("V", [3, 16, 300, 9001])
 def test_distill_entries(torch, emo, K, V):
