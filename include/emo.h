@@ -386,7 +386,10 @@ emo_status emo_graph_set_timing_events(emo_graph_t g, void *begin_event, void *e
  * operand, except that the adjusted logits or the gradient may be the logits themselves (same data,
  * type, rows and strides).
  * An operand passed as NULL is absent.  Data outside an operand's rows and columns (between strided
- * rows, behind the last) is not written.
+ * rows, behind the last) is not written, so an output may lie between another operand's rows: columns,
+ * or parts of the rows, of one buffer.  Operands whose first to last bytes meet are taken to be apart
+ * where their rows, or else their elements, keep to places apart in every stretch of bytes as long as
+ * the greatest common divisor of their row strides (or else of all their strides), and refused otherwise.
  */
 typedef enum {
     EMO_F32 = 0,

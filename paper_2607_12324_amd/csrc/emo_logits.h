@@ -6,6 +6,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <numeric>
 #include <type_traits>
 
 #include "emo_internal.h"
@@ -401,6 +402,8 @@ struct Checker {
         uintptr_t begin, end;
         bool output;
         const emo_tensor *t;
+        int64_t size;                   // bytes of an element (a workspace is one)
+        int64_t stride[2], width[2];    // bytes from a row to the next and of a row, and those of the columns (strides of one: 0)
     } ranges[16];
     int n = 0;
     int last = -1;      // the range of the operand taken last, -1 if it has none
@@ -451,7 +454,11 @@ struct Checker {
         m.data = static_cast<const char *>(t->data);
         if (n < 16) {
             last = n;
-            ranges[n++] = {name, p, p + static_cast<uintptr_t>((static_cast<int64_t>(end) + 1) * size), output, t};
+            Range &g = ranges[n++];
+            g = {name, p, p + static_cast<uintptr_t>((static_cast<int64_t>(end) + 1) * size), output, t, size,
+                 {t->rows > 1 ? t->row_stride * size : 0, t->cols > 1 ? t->col_stride * size : 0}, {}};
+            g.width[0] = (t->cols - 1) * g.stride[1] + size;
+            g.width[1] = (t->rows - 1) * g.stride[0] + size;
         }
         return m;
     }
@@ -462,7 +469,24 @@ struct Checker {
             return bad(fail(EMO_ERR_INVALID_ARGUMENT, "workspace of %lld bytes, needs %lld", (long long)(p ? have : 0), (long long)need));
         const uintptr_t b = reinterpret_cast<uintptr_t>(p);
         if (b % 16) return bad(fail(EMO_ERR_INVALID_ARGUMENT, "workspace is not 16-byte aligned"));
-        if (n < 16) ranges[n++] = {"workspace", b, b + static_cast<uintptr_t>(need), true, nullptr};
+        if (n < 16) ranges[n++] = {"workspace", b, b + static_cast<uintptr_t>(need), true, nullptr, need, {0, 0}, {need, need}};
+    }
+
+    // Whether two ranges that meet share no byte.  Every row (or column) of either begins a multiple of `unit` behind its
+    // first, so that what they take of each `unit` bytes is one interval; it is checked that the two intervals are apart.
+    // So are columns of one buffer and parts of its rows; with `unit` from all strides, elements by turns.
+    static bool between(const Range &x, const Range &y) {
+        const uint64_t ahead = x.begin <= y.begin ? y.begin - x.begin : x.begin - y.begin;
+        const auto apart_in = [&](int64_t unit, int64_t x_width, int64_t y_width) {
+            if (unit == 0) return false;
+            const int64_t rest = static_cast<int64_t>(ahead % static_cast<uint64_t>(unit));
+            const int64_t from_x = x.begin <= y.begin || rest == 0 ? rest : unit - rest;      // to the next interval of y
+            return x_width <= from_x && y_width <= unit - from_x;
+        };
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2; ++j)
+                if (apart_in(std::gcd(x.stride[i], y.stride[j]), x.width[i], y.width[j])) return true;
+        return apart_in(std::gcd(std::gcd(x.stride[0], x.stride[1]), std::gcd(y.stride[0], y.stride[1])), x.size, y.size);
     }
 
     // Outputs lie apart from everything else; the output of range `twin` may be the very memory of range `of`
@@ -476,6 +500,7 @@ struct Checker {
                 if (i == twin && j == of && x->data == y->data && x->dtype == y->dtype && x->rows == y->rows && x->cols == y->cols &&
                     (x->rows == 1 || x->row_stride == y->row_stride))
                     continue;
+                if (between(ranges[i], ranges[j])) continue;
                 return status = fail(EMO_ERR_INVALID_ARGUMENT, "%s overlaps %s", ranges[i].name, ranges[j].name);
             }
         return EMO_OK;

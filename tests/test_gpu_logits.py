@@ -707,6 +707,42 @@ def test_streams_and_graphs(torch, emo):
     assert torch.equal(c, want[0][1]) and torch.equal(l, want[0][2]) and torch.equal(s, want[0][3])
 
 
+@pytest.mark.parametrize("V", [8, 40, 300, 9001, 70001])
+def test_outputs_beside_each_other(torch, emo, V):
+    """Outputs as columns of one buffer, between the rows of the logits, beside the noise: the values of the same
+    call on memory of its own, and nothing else written."""
+    N, K = 5, 6
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(V)
+    I = torch.randint(0, V, (N, K), generator=gen, device="cuda", dtype=torch.int32)
+    T = torch.randn((N, K), generator=gen, device="cuda")
+    both = torch.randn((N, 2 * V + 1), generator=gen, device="cuda")
+    X, Y = both[:, :V], both[:, V + 1:]
+    alone = X.contiguous()
+    loss, stats = emo.distill_forward(alone, I, T)
+    kept = torch.full((N, 4), 7.0, device="cuda")
+    emo.distill_forward(X, I, T, loss=kept[:, 0], stats=kept[:, 2:])
+    assert torch.equal(kept[:, 0], loss) and torch.equal(kept[:, 2:], stats) and bool((kept[:, 1] == 7).all())
+    want = emo.distill_backward(alone, stats, I, T)
+    emo.distill_backward(X, stats, I, T, grad=Y)
+    assert torch.equal(Y, want) and torch.equal(X, alone)
+    loss, want = emo.distill_step(alone, I, T)
+    wide = torch.cat([both, both.new_full((N, 1), 7.0)], 1)
+    X, Y = wide[:, :V], wide[:, V:2 * V]
+    emo.distill_step(X, I, T, loss=wide[:, 2 * V + 1], grad=Y)
+    assert torch.equal(Y, want) and torch.equal(wide[:, 2 * V + 1], loss) and torch.equal(X, alone)
+    assert torch.equal(wide[:, 2 * V], both[:, 2 * V])
+    # the adjusted logits in the noise's buffer, the choice in the last column of another
+    noise = torch.randn((N, V), generator=gen, device="cuda")
+    mixed = torch.cat([noise, noise], 1)
+    chosen = torch.full((N, V + 2), 7, dtype=torch.int32, device="cuda")
+    want, wc = emo.adjust_logits(alone, noise=noise, out=torch.empty_like(alone),
+                                 choice=torch.empty(N, dtype=torch.int32, device="cuda"))
+    emo.adjust_logits(alone, noise=mixed[:, :V], out=mixed[:, V:], choice=chosen[:, V])
+    assert torch.equal(mixed[:, V:], want) and torch.equal(mixed[:, :V], noise) and torch.equal(chosen[:, V], wc)
+    assert bool((chosen[:, :V] == 7).all()) and bool((chosen[:, V + 1] == 7).all())
+
+
 def test_offsets_past_32_bits(torch, emo):
     """Rows whose first elements lie beyond 2^31 elements and 2^32 bytes."""
     N, V, stride = 3, 1000, (1 << 30) + 4099

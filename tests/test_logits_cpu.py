@@ -194,6 +194,56 @@ def test_distill_in_place_frees_no_other_operand(emo, mem):
             refused(emo, backward(emo, N, V, t, stats=mem(N, 2), grad=grad), "gradient overlaps teacher")
 
 
+def test_outputs_between_the_rows_of_others(emo, mem):
+    """What shares no byte is no overlap.  Another type than the logits' in the output, looked for after the
+    overlaps, keeps the accepted layouts from being run."""
+    R, V, at = 6, 100, 1 << 33
+
+    def out(logits, data, row_stride, words, rows=R, **kw):
+        t = emo.Tensor(data, rows, V, row_stride, 1, F16, 0)
+        refused(emo, adjust(emo, rows, V, logits=logits, out=t, **kw), *words)
+
+    apart, meet = ("out must have the logits' type",), ("out overlaps",)
+    half = emo.Tensor(at, R, V, 2 * V, 1, F32, 0)
+    out(half, at + 4 * V, 4 * V, apart)                             # the right half of the logits' rows
+    out(half, at + 6 * V, 4 * V, apart)                             # its last 2 V bytes
+    out(half, at + 6 * V + 2, 4 * V, meet)                          # 2 bytes into the next row's logits
+    out(half, at + 4 * V - 2, 4 * V, meet)
+    out(half, at - 4 * V, 4 * V, apart)                             # the half before the first row
+    out(half, at - 2 * V, 4 * V, apart)
+    out(half, at - 2 * V + 2, 4 * V, meet)
+    out(half, at + 4 * V, 4 * V + 2, meet)                          # the strides drift
+    out(half, at + 4 * V, 8 * V, apart)                             # every other row's right half
+    out(half, at + 4 * V, 2 * V, meet)                              # twice as many rows as the buffer's
+    out(emo.Tensor(at, 1, V, V, 1, F32, 0), at + 4 * V, 4 * V, apart)
+    out(emo.Tensor(at, 1, V, V, 1, F32, 0), at - 4 * V, 4 * V, apart)   # one row in the others' gap
+    out(emo.Tensor(at, 1, V, V, 1, F32, 0), at - 2 * V, 4 * V, apart)
+    out(emo.Tensor(at, 1, V, V, 1, F32, 0), at - 2 * V + 2, 4 * V, meet)
+    out(emo.Tensor(at, 1, V, V, 1, F32, 0), at, 4 * V, meet)
+    # a history read through a transposed view of the buffer's last rows, and one that the output's rows cross
+    half16 = emo.Tensor(at, R, 9, 1, 4 * V, I32, 0)
+    rate = mem(R, 1)
+    out(mem(R, V), at + 64, 8 * V, apart, history=half16, presence=rate)
+    out(mem(R, V), at + 20, 8 * V, meet, history=half16, presence=rate)
+    # the elements of two by turns
+    turns = emo.Tensor(at, R, 9, 18, 2, I32, 0)
+    choice = emo.Tensor(at + 4, R, 1, 18, 1, I32, 0)
+    refused(emo, adjust(emo, R, V, logits=mem(R, V), history=turns, presence=rate, choice=choice, out=mem(R, V, F16)), *apart)
+    choice = emo.Tensor(at + 8, R, 1, 18, 1, I32, 0)
+    refused(emo, adjust(emo, R, V, logits=mem(R, V), history=turns, presence=rate, choice=choice, out=mem(R, V, F16)), "choice overlaps")
+    # a workspace among the elements of a strided column, and in the gap between two rows
+    long, n = 1 << 22, ctypes.c_int64(0)
+    assert emo.lib.emo_adjust_workspace(R, long, ctypes.byref(n)) == 0 and n.value > 64
+    kw = {"logits": mem(R, long), "ws": at, "size": n.value}
+    refused(emo, adjust(emo, R, long, choice=emo.Tensor(at + 8, R, 1, 2, 1, I64, 0), **kw), "overlaps")
+    refused(emo, adjust(emo, R, long, choice=emo.Tensor(at - 8, R, 1, (n.value + 15) // 8, 1, I64, 0), out=mem(R, long, F16), **kw), *apart)
+    t = {"logits": half, "ids": mem(R, 5, I32), "teacher": mem(R, 5)}
+    for data, words in ((at + 4 * V, "type"), (at + 4 * V - 2, "overlaps")):
+        g = emo.Tensor(data, R, V, 4 * V, 1, F16, 0)
+        refused(emo, step(emo, R, V, t, loss=mem(R, 1), grad=g), words)
+        refused(emo, backward(emo, R, V, t, stats=mem(R, 2), grad=g), words)
+
+
 def test_workspaces(emo, mem):
     n = ctypes.c_int64(-1)
     for fn in (emo.lib.emo_adjust_workspace, emo.lib.emo_distill_workspace):
