@@ -419,6 +419,7 @@ struct Checker {
         if (!t || status != EMO_OK) return m;
         if (t->dtype < EMO_F32 || t->dtype > EMO_I64 || !(types & bit(t->dtype)))
             return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s has a type that this call does not take (%d)", name, (int)t->dtype)), m;
+        if (t->reserved != 0) return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s has a reserved field that is not 0", name)), m;
         if (cols >= 0 && t->cols != cols)
             return bad(fail(EMO_ERR_INVALID_ARGUMENT, "%s has %lld columns, needs %lld", name, (long long)t->cols, (long long)cols)), m;
         if (t->cols < 0 || t->cols >= kMaxRows || t->rows < 0 || t->rows >= kMaxRows)

@@ -104,6 +104,19 @@ def test_adjust_refuses(emo, mem):
     refused(emo, adjust(emo, R, 256, logits=mem(R, 256), choice=mem(R, 1, U8)), "byte")
 
 
+def test_reserved_fields_are_zero(emo, mem):
+    """A record that was not cleared is refused, whichever operand it is."""
+    R, V = 6, 100
+    W = (V + 31) // 32
+    kw = {"logits": mem(R, V), "history": mem(R, 9, I32), "lengths": mem(R, 1, I32), "repetition": mem(R, 1), "frequency": mem(R, 1),
+          "presence": mem(R, 1), "bias": mem(1, V), "inv_temperature": mem(R, 1), "mask": mem(R, W, I32), "noise": mem(R, V),
+          "out": mem(R, V), "choice": mem(R, 1, I32)}
+    for k, t in kw.items():
+        t.reserved = 1
+        refused(emo, adjust(emo, R, V, **kw), k, "reserved")
+        t.reserved = 0
+
+
 def test_adjust_refuses_overlaps(emo, mem):
     R, V = 6, 100
     x = mem(R, V)
