@@ -121,6 +121,7 @@ __device__ __forceinline__ void load_values(const Mat &m, uint32_t row, int32_t 
 // Entries of a row that a lane holds at once: 16 bytes of logits, loaded at any alignment of the type (rows
 // of an odd count start anywhere; the hardware takes 16-byte accesses at such addresses).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2), may_alias));
 template <typename T>
@@ -261,8 +262,14 @@ __device__ __forceinline__ void load_floats_once(const float *row, int32_t v, in
 
 // Wide rows are written as a stream, which the caches pass on: kept, they drive out what other workgroups still
 // read (256 x 131,072 bf16 adjusted: 33 us against 40; 517 x 50,021 fp32, a step: 65 against 70).
-template <bool Stream, typename V>
-__device__ __forceinline__ void store_words(V *to, const V &raw) {
+// (Two functions: a template's parameter would be the type without its alignment of 2.)
+template <bool Stream>
+__device__ __forceinline__ void store_words(u32x4_any *to, u32x4 raw) {
+    if constexpr (Stream) __builtin_nontemporal_store(raw, to);
+    else *to = raw;
+}
+template <bool Stream>
+__device__ __forceinline__ void store_words(u32x2_any *to, u32x2 raw) {
     if constexpr (Stream) __builtin_nontemporal_store(raw, to);
     else *to = raw;
 }
@@ -274,16 +281,15 @@ __device__ __forceinline__ void store_chunk(O *row, int32_t v, const float (&f)[
         for (int i = 0; i < N; i += 4) {
             u32x4 raw;
             for (int j = 0; j < 4; ++j) raw[j] = __float_as_uint(f[i + j]);
-            store_words<Stream>(reinterpret_cast<u32x4_any *>(at_entry(row, v) + i), u32x4_any(raw));
+            store_words<Stream>(reinterpret_cast<u32x4_any *>(at_entry(row, v) + i), raw);
         }
     } else if constexpr (N == 4) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
         const u32x2 raw = {pack_two<O>(f[0], f[1]), pack_two<O>(f[2], f[3])};
-        store_words<Stream>(reinterpret_cast<u32x2_any *>(at_entry(row, v)), u32x2_any(raw));
+        store_words<Stream>(reinterpret_cast<u32x2_any *>(at_entry(row, v)), raw);
     } else {
         u32x4 raw;
         for (int w = 0; w < 4; ++w) raw[w] = pack_two<O>(f[2 * w], f[2 * w + 1]);
-        store_words<Stream>(reinterpret_cast<u32x4_any *>(at_entry(row, v)), u32x4_any(raw));
+        store_words<Stream>(reinterpret_cast<u32x4_any *>(at_entry(row, v)), raw);
     }
 }
 

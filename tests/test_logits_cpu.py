@@ -1,6 +1,8 @@
 """The calls on logits without a GPU: what they refuse (nothing is launched, the addresses passed are
 never read), and that empty calls are fine."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -304,3 +306,13 @@ def test_binding_refuses_host_tensors(emo):
     with pytest.raises(ValueError, match="rows"):
         emo.adjust_logits(x[0])
     assert ctypes.sizeof(emo.Tensor) == 48 and np.dtype(np.int64).itemsize == 8
+
+
+@pytest.mark.parametrize("source", ["emo_logits.hip", "emo_distill.hip"])
+def test_no_access_claims_an_alignment_that_rows_lack(source):
+    """Rows start at any element: a pointer into one is never taken for a more aligned one."""
+    from paper_2607_12324_amd import build as b
+    cmd = [os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *b.HIPCC_FLAGS, "-I", b.INCLUDE, "-I", b.CSRC, "--cuda-device-only",
+           "-fsyntax-only", "-Werror=align-mismatch", os.path.join(b.CSRC, source)]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-2000:]
