@@ -156,6 +156,24 @@ def test_adjust_rows(torch, emo, R, V, distinct):
     check_adjust(torch, emo, rng, R, V, "bf16", "f32", choice="", distinct=distinct, mask=1, bias=1, L=33)
 
 
+@pytest.mark.parametrize("V", [(1 << 20) + 1, 3 * (1 << 20) + 77])
+def test_adjust_choices_among_more_than_256_tiles(torch, emo, V):
+    """Ties of the greatest value in tiles far apart, in a tile, at a row's ends; none; noise on all of it."""
+    rng = np.random.default_rng(V)
+    x = np.minimum(rng.normal(size=(6, V)).astype(np.float32), np.float32(4))
+    far = 4096 * 255
+    for r, at in enumerate(([far + 7, far - 1], [V - 1, far + 1], [V - 1], [0, V - 1, far], [], [])):
+        x[r, at] = 9.0
+    x[4] = np.nan
+    for kw in ({}, {"noise": rng.gumbel(size=(1, V)).astype(np.float32)}):
+        _, wc = orc.adjust(6, x, **kw)
+        C = torch.empty(6, dtype=torch.int64, device="cuda")
+        emo.adjust_logits(dev(torch, x), choice=C, **{k: dev(torch, v) for k, v in kw.items()})
+        assert C.cpu().tolist() == wc.tolist()
+        if not kw:
+            assert wc[:5].tolist() == [far - 1, far + 1, V - 1, 0, -1]
+
+
 @pytest.mark.parametrize("L", [0, 1, 2, 63, 64, 65, 1000, 5000, 70000])
 @pytest.mark.parametrize("V", [6, 200, 3000, 30011])
 def test_adjust_histories(torch, emo, L, V):
@@ -542,6 +560,42 @@ def test_distill_many_rows(torch, emo, N, V, dtype):
     assert bool(((loss - loss2).abs() <= near * (1 + loss.abs())).all())
     q = g.float().abs() + 1e-3
     assert bool(((g.float() - g2.float()).abs() <= q * (near + 2 * HALF[dtype])).all())
+
+
+@pytest.mark.parametrize("V", [65537, 100003, 131072])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_distill_widest_rows_held(torch, emo, V, dtype):
+    """Rows of 65,537 to 131,072 2-byte entries that a workgroup holds: more than 32 of them."""
+    rng = np.random.default_rng(V)
+    check_distill(torch, emo, rng, 33, V, 40, dtype, mask=1, scaled=False)
+    check_distill(torch, emo, rng, 34, V, 20, dtype, "i64", grad="f32", stride=V + 3, offset=1)
+    check_distill(torch, emo, rng, 35, V, 7, dtype, mask=35, tau=2.0, in_place=True)
+
+
+@pytest.mark.parametrize("N,V,dtype", [(4200, 2049, "bf16"), (4200, 4096, "f16"), (8300, 2500, "f32")])
+def test_distill_many_rows_of_long_lists(torch, emo, N, V, dtype):
+    """More rows than the card holds at once with lists longer than a sixteenth of the row: a wave a row and a
+    table of probabilities.  Against the two passes on every row, the oracle on some."""
+    rng = np.random.default_rng(N)
+    K = 300
+    x = torch.from_numpy(rng.normal(size=(N, V)).astype(np.float32) * 3).to(types(torch)[dtype])
+    i, t = rng.integers(-1, V, size=(N, K)), rng.normal(size=(N, K)).astype(np.float32)
+    i[:, 100:200] = rng.integers(0, 3, size=(N, 100)) * (V // 2)
+    words = orc.mask_words(rng.random((1, V)) < 0.8)
+    X, I, T, M = x.cuda(), dev(torch, i, "i32"), dev(torch, t), dev(torch, words)
+    loss, stats = emo.distill_forward(X, I, T, mask=M)
+    g = emo.distill_backward(X, stats, I, T, mask=M)
+    loss2, g2 = emo.distill_step(X, I, T, mask=M)
+    some = rng.choice(N, 6, replace=False)
+    w = orc.distill(x.float().numpy()[some], i[some], t[some], 1.0, words)
+    _, tl, tg = bounds(w, V, K, 1.0, np.ones(6), dtype)
+    for a, b in ((loss, g), (loss2, g2)):
+        check_near(a.cpu().numpy()[some], w["loss"], tl, "loss")
+        check_near(b.float().cpu().numpy()[some], w["grad"], tg, "gradient")
+    # the two differ by their roundings: of s and, at an entry's summed probability, of the list
+    near = 2 * (V / 256 + 67 + 60 + K + 8) * EPS
+    assert bool(((loss - loss2).abs() <= near * (1 + loss.abs())).all())
+    assert bool(((g.float() - g2.float()).abs() <= (g.float().abs() + 1e-3) * (near + 2 * HALF[dtype])).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
