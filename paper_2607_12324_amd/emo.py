@@ -8,7 +8,6 @@ raises at import time; there is no fallback.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 import struct
 from dataclasses import dataclass
