@@ -182,6 +182,14 @@ def test_adjust_histories(torch, emo, L, V):
     check_adjust(torch, emo, rng, 2, V, "f32", "f32", L=L, ids="u8" if V <= 200 else "i64", lengths=False, noise=2)
 
 
+@pytest.mark.parametrize("L", [2048, 2049, 6000])
+@pytest.mark.parametrize("R,V", [(300, 8193), (3, 8193), (3, 32769), (5, 100003), (1, 1 << 20)])
+def test_adjust_long_histories_of_wide_rows(torch, emo, R, V, L):
+    rng = np.random.default_rng(V + L)
+    check_adjust(torch, emo, rng, R, V, "bf16", "f32", L=L, ids="i32", mask=1, bias=1)
+    check_adjust(torch, emo, rng, min(R, 3), V, "f16", "f16", L=L, ids="i64", choice="", in_place=True, stride=V + 3, offset=1)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("V", [9, 64, 1031, 50021])
 def test_adjust_in_place_and_strides(torch, emo, dtype, V):
