@@ -240,8 +240,10 @@ __device__ __forceinline__ Running block_stats(const Running &run, float log2e_t
 }
 
 // What a workgroup holds of a row: n entries from v0 on, those of whole chunks 16 bytes a lane, the rest (fewer
-// than a chunk) an entry a lane.  Masked entries are -infinity.  Once: the logits are not read again (forward
-// 2,048 x 131,072 bf16: 99 us against 104 without the hint; backward 199 with it against 187).
+// than a chunk) an entry a lane.  Masked entries are -infinity.  Once: a hint that the logits are not read again.  The
+// forward pass has it (2,048 x 131,072 bf16: 92 us against 103 without; 1,024 x 50,021 fp32 42 against 46; rows that the
+// caches hold from call to call lose: 4,096 x 8,000 bf16 22 against 19), the backward pass has not (183 us against 190
+// with it; 88 against 83; 32 against 36).
 template <typename T, int Threads, int C, bool Once>
 struct Piece {
     static constexpr bool Early = C <= 8;       // longer rows have no registers to hold the mask's bytes meanwhile: LDS does
@@ -267,8 +269,8 @@ struct Piece {
 };
 
 // Forward: a workgroup per part of a row (`span` entries, a multiple of what it holds at once).  Bound by
-// memory: the next Threads * 32 entries are loaded while these are added (2,048 x 131,072 bf16: 91 us, 5.9 TB/s,
-// what a sum over 1 GiB reaches).  A row of one part is finished here,
+// memory: the next Threads * 32 entries are loaded while these are added (2,048 x 131,072 bf16: 92 us, 5.9 TB/s,
+// what a sum over 1 GiB reaches; 4,000 rows 162 us, 6.5 TB/s).  A row of one part is finished here,
 // others leave their statistics to finish_kernel.
 template <typename T, int Threads>
 __global__ void __launch_bounds__(Threads) forward_kernel(DistillArgs a, uint32_t first, Pieces pieces, int32_t span, float2 *partial) {
@@ -402,7 +404,7 @@ __global__ void __launch_bounds__(Threads) backward_kernel(DistillArgs a, uint32
 }
 
 // Loss and gradient of rows that fit a workgroup's registers: read once, written once (8,192 x 32,768 bf16:
-// 196 us, 5.5 TB/s; the forward and the backward kernel one after the other take half as long again).
+// 197 us, 5.5 TB/s; the forward and the backward kernel one after the other take half as long again).
 template <typename T, typename O, int Threads, int PerThread>
 __global__ void __launch_bounds__(Threads) step_kernel(DistillArgs a, int64_t first) {
     constexpr int C = PerThread / kChunk<T>;
@@ -680,7 +682,8 @@ __global__ void __launch_bounds__(kThreads) small_kernel(SmallArgs a, int64_t fi
 // ------------------------------------------------------------------------------ launches
 
 // The parts of a row of the forward pass: of whole 8,192 entries, as many as bring 2,048 workgroups (8 a
-// compute unit) while a row has that many.
+// compute unit) while a row has that many.  More rows than that fill the card unsplit: split up to 4,096 workgroups,
+// 2,049 rows of 131,072 bf16 took 94 us against 92, 3,000 131 against 124, 3,000 rows of 32,768 42 against 36.
 struct Parts {
     int32_t parts, span;
 };
