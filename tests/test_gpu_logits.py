@@ -826,6 +826,116 @@ def test_offsets_past_32_bits(torch, emo):
     check_near(g.float().cpu().numpy(), w["grad"], tg, "gradient")
 
 
+@pytest.mark.parametrize("tau", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 60])
+@pytest.mark.parametrize("V", [9, 300, 9001, 70001])
+def test_distill_temperatures_at_their_limits(torch, emo, V, tau):
+    rng = np.random.default_rng(V)
+    check_distill(torch, emo, rng, 3, V, 12, tau=tau, mask=1)
+    check_distill(torch, emo, rng, 3, V, 5, "bf16", tau=tau, grad="f32", scaled=False)
+
+
+def test_calls_of_several_launches(torch, emo):
+    """More workgroups than a launch takes (2^21): the last rows are what they are alone."""
+    rng = np.random.default_rng(0)
+    N, V, K = (1 << 21) + 5, 70, 3
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    X = torch.randn((N, V), generator=gen, device="cuda").bfloat16()
+    I = torch.randint(0, V, (N, K), generator=gen, device="cuda", dtype=torch.int32)
+    T = torch.randn((N, K), generator=gen, device="cuda")
+    loss, stats = emo.distill_forward(X, I, T)
+    g = emo.distill_backward(X, stats, I, T)
+    loss2, g2 = emo.distill_step(X, I, T)
+    C = torch.empty(N, dtype=torch.int64, device="cuda")
+    O, _ = emo.adjust_logits(X, history=I, presence=T[:1, 0], out=torch.empty_like(X), choice=C)
+    for rows in (slice(0, 3), slice((1 << 21) - 2, N)):
+        x, i, t = X[rows].float().cpu().numpy(), I[rows].cpu().numpy(), T[rows].cpu().numpy()
+        w = orc.distill(x, i, t, 1.0)
+        _, tl, tg = bounds(w, V, K, 1.0, np.ones(len(x)), "bf16")
+        for a, b in ((loss, g), (loss2, g2)):
+            check_near(a[rows].cpu().numpy(), w["loss"], tl, "loss")
+            check_near(b[rows].float().cpu().numpy(), w["grad"], tg, "gradient")
+        want, wc = orc.adjust(len(x), x, history=i, presence=T[:1, 0].cpu().numpy())
+        bits_equal(torch, O[rows], want, "bf16", "adjusted")
+        assert C[rows].cpu().tolist() == wc.tolist()
+    del X, I, T, g, g2, O
+    # rows of several tiles, choices joined; 3 rows of logits in turn
+    R, V = (1 << 21) + 1, 16400
+    x = rng.normal(size=(3, V)).astype(np.float32)
+    C = torch.empty(R, dtype=torch.int32, device="cuda")
+    emo.adjust_logits(dev(torch, x), rows=R, choice=C)
+    assert R % 3 == 0 and bool((C.view(-1, 3) == torch.from_numpy(orc.adjust(3, x)[1]).cuda()).all())
+    # rows of a few entries
+    N, V, K = (1 << 27) + 70, 4, 5
+    x, i, t = rng.normal(size=(1, V)).astype(np.float32), rng.integers(0, V, size=(1, K)), rng.normal(size=(1, K)).astype(np.float32)
+    loss, g = emo.distill_step(dev(torch, x).expand(N, V), dev(torch, i, "i32"), dev(torch, t))
+    w = orc.distill(x, i, t, 1.0)
+    _, tl, tg = bounds(w, V, K, 1.0, np.ones(1), "f32")
+    check_near(loss[:1].cpu().numpy(), w["loss"], tl, "loss")
+    check_near(g[:1].cpu().numpy(), w["grad"], tg, "gradient")
+    assert bool((loss == loss[0]).all()) and bool((g == g[0]).all())
+
+
+@pytest.mark.parametrize("V", [5, 300, 9001])
+def test_counts_past_24_bits(torch, emo, V):
+    """One id (2^24 + 3 times, read at a column stride of 0): the count is rounded to fp32 as the oracle's is."""
+    L = (1 << 24) + 3
+    x = np.random.default_rng(V).normal(size=(2, V)).astype(np.float32)
+    h, rate = np.array([[V - 1], [2]]), np.float32([1.0, 0.37])
+    want, wc = orc.adjust(2, x, history=np.broadcast_to(h, (2, L)), frequency=rate)
+    O, C = emo.adjust_logits(dev(torch, x), history=dev(torch, h, "i32").expand(2, L), frequency=dev(torch, rate),
+                             out=torch.empty((2, V), device="cuda"), choice=torch.empty(2, dtype=torch.int32, device="cuda"))
+    bits_equal(torch, O, want, "f32", "adjusted")
+    assert C.cpu().tolist() == wc.tolist() and want[0, V - 1] < -1.6e7
+
+
+def test_nearly_2_31_rows(torch, emo):
+    """Candidates for 2,047 packs, 2^20 of them: row r reads row r % 2047 up to the last."""
+    P, B, V = 2047, 1 << 20, 8
+    x = np.random.default_rng(3).normal(size=(P, V)).astype(np.float32)
+    C = torch.full((B * P,), 77, dtype=torch.uint8, device="cuda")
+    emo.adjust_logits(dev(torch, x), rows=B * P, choice=C)
+    want = torch.from_numpy(orc.adjust(P, x)[1]).to(torch.uint8).cuda()
+    for part in C.view(B, P).split(B // 8):
+        assert bool((part == want).all())
+
+
+def test_nearly_2_31_entries(torch, emo):
+    """A row of 2^31 - 1 entries: indexes, offsets and sums to its end."""
+    V = (1 << 31) - 1
+    far = [V - 1, (1 << 30) + 3, 7]
+    X = torch.zeros((1, V), dtype=torch.bfloat16, device="cuda")
+    X[0, far] = 4.0
+    X[0, V // 2] = 3.0
+    words = torch.full((1, (V + 31) // 32), -1, dtype=torch.int32, device="cuda")
+    C = torch.empty(1, dtype=torch.int32, device="cuda")
+    assert int(emo.adjust_logits(X, choice=C)[1]) == 7
+    words[0, 0] &= ~(1 << 7)
+    assert int(emo.adjust_logits(X, mask=words, choice=C)[1]) == (1 << 30) + 3
+    H = torch.tensor([[V - 1, far[1], -1, V - 1, 9]], device="cuda")
+    rate = torch.tensor([1.5], device="cuda")
+    O, _ = emo.adjust_logits(X, history=H, presence=rate, frequency=rate, mask=words, out=torch.empty_like(X), choice=C)
+    assert int(C) == V // 2
+    assert O[0, [V - 1, far[1], 7, 9, 8, V - 2]].tolist() == [-0.5, 1.0, -float("inf"), -3.0, 0.0, 0.0]
+    del O
+    I = torch.tensor([[V - 1, 12, V // 2]], device="cuda")
+    T = torch.tensor([[1.0, 0.0, 2.0]], device="cuda")
+    loss, stats = emo.distill_forward(X, I, T)
+    s = 3 + np.exp(-1.0) + (V - 4) * np.exp(-4.0)
+    p = np.exp([1.0, 0.0, 2.0]) / np.exp([1.0, 0.0, 2.0]).sum()
+    near = (8 + 4 + 128 + 6 + 4 + 32 + 6 + 16) * EPS        # chunks, steps, a wave, waves, a row's parts, a wave; the exponents
+    check_near(stats.cpu().numpy(), np.array([[4.0, s]]), np.array([[0.0, near * s]]), "statistics")
+    want = np.log(s) + (p * [0.0, 4.0, 1.0]).sum()
+    check_near(loss.cpu().numpy(), np.array([want]), near + 16 * EPS * want, "loss")
+    for g in (emo.distill_backward(X, stats, I, T), emo.distill_step(X, I, T, grad=X)[1]):
+        at = [V - 1, 12, V // 2, far[1], 7, 0, V - 2]
+        q = np.exp([0.0, -4.0, -1.0, 0.0, 0.0, -4.0, -4.0]) / s
+        w = q - np.concatenate([p, np.zeros(4)])
+        check_near(g[0, at].float().cpu().numpy(), w, np.abs(w) * (near + 2 * HALF["bf16"]), "gradient")
+        others = sum(int((part != g[0, 0]).sum()) for part in g[0].split(1 << 28))
+        assert others == 5          # all but the teacher's entries and the three greatest
+
+
 def test_a_learned_search(torch, emo):
     """The calls together, as a search uses them: levels drawn from the packs' logits under a mask, evaluated
     where they lie, the best candidates' levels as the teacher; each step against the oracle."""
