@@ -365,7 +365,7 @@ bool small_rows(const AdjustArgs &a, GroupArgs *g) {
 // A row's tiles: one of 2,048 entries by a wave; longer rows of 4,096 by 256 threads (2 x 2^20 entries: 5.7 us,
 // tiles of 2,048 by single waves 7.7).  A tile looks through its row's whole history, so a long one wants more
 // threads and fewer tiles: past 512 ids a row of a wave's goes to 256 threads (12 rows of 650 with 6,707 ids: 11.5 us,
-// 22 by a wave), past 2,048 every row to 512 threads with tiles of 8,192 (12 rows of 650: 9.1; 300 rows of 7,000 with
+// 22 by a wave), past 2,048 every row but those below to 512 threads with tiles of 8,192 (12 rows of 650: 9.1; 300 rows of 7,000 with
 // 4,000 ids: 10, 18 by 256 threads; 1,000 x 32,000 bf16 with up to 4,096 ids: 48 against 60, with 8,192 ids 66
 // against 86; 333 x 100,003 fp16: 56 against 57, 69 against 75; one row of 2^20 13 against 16; the other way only where
 // many rows fill little of a tile: 1,112 rows of 992 with 7,467 ids 18, 16 by 256 threads).
